@@ -333,6 +333,125 @@ typedef struct {
  * replayed.                                                                                     */
 int co3_ps_aggregate(const co3_plan *plan, const co3_aggregate_args *args, void *stream);
 
+/* ---- training around the codec -----------------------------------------------------------
+ * What makes the gradient that is coded and what is made of its average.  Tensors are device
+ * memory in one of these types; statistics, momentum, model and weight gradients are fp32.     */
+enum { CO3_F32 = 0, CO3_BF16 = 1, CO3_F16 = 2 };
+
+/* Matrices of the flat vector: row r, column c of a matrix is element offset + r ld + c.  They may
+ * lie at any offset and in any order, side by side in the same rows too, and must not overlap.    */
+typedef struct {
+    uint64_t offset;
+    uint64_t ld;             /* elements between rows, >= cols                                 */
+    uint32_t rows, cols;     /* 1 .. 2^20 each                                                 */
+    float scale;             /* factor of the orthogonalised matrix, finite                    */
+    int32_t reserved;
+} co3_matrix;
+
+typedef struct co3_matrix_plan co3_matrix_plan;   /* layout of a set of matrices: library-owned  */
+
+/* How the products of fp16 operands are formed (every sum is fp32).  An operand is a pair hi + lo of fp16
+ * numbers, 22 bits.  CO3_PRODUCTS_PAIR multiplies hi hi + hi lo + lo hi: the results have about fp32's
+ * precision.  CO3_PRODUCTS_HIGH multiplies the high parts only, at a third of the work: errors of about
+ * 2e-3 of the result, the size of its rounding to bf16.  The iterate itself stays a pair either way, so that
+ * what the steps amplify is not the rounding.                                                         */
+enum { CO3_PRODUCTS_PAIR = 0, CO3_PRODUCTS_HIGH = 1 };
+
+/* count matrices of a vector of `type` (co3_muon_update takes CO3_F32).  Allocates small device tables;
+ * synchronises the device.  Errors: CO3_ERR_ARG for a null pointer, no matrices or more than 65536, a size, an
+ * ld, a scale, a type or products outside the above, matrices that overlap; CO3_ERR_CAPACITY where the host's
+ * memory, or the 2^31 - 1 tiles of a launch, do not suffice.                                            */
+int co3_matrix_plan_create(uint32_t count, const co3_matrix *matrices, int32_t type, int32_t products,
+                           co3_matrix_plan **out);
+void co3_matrix_plan_destroy(co3_matrix_plan *plan);
+size_t co3_matrix_plan_workspace_bytes(const co3_matrix_plan *plan);
+uint64_t co3_matrix_plan_elements(const co3_matrix_plan *plan);   /* the vector's least length   */
+
+/* Newton-Schulz iteration.  X = G, or its transpose where G has more rows than columns:
+ *   X_0 = X / (|X|_F + eps);   A = X_k X_k^T,  X_{k+1} = a_k X_k + (b_k A + c_k A A) X_k;   out = scale X_steps
+ * coefficients: host [steps][3] = (a_k, b_k, c_k), read before the call returns.  Singular values lie in [0, 1] at
+ * first; the polynomials have to keep them in [0, 2], and |b s^2 + c s^4| <= 7 there (CO3_ERR_ARG).  A matrix
+ * of zeros gives zeros.  A matrix with a norm that is not finite gives NaN throughout and is counted in
+ * status[CO3_STAT_NONFINITE].  g and out: the vector, of the plan's type, aligned as its elements are; out may
+ * be g.  Elements outside the matrices are neither read nor written.                                      */
+#define CO3_MAX_NS_STEPS 32u
+typedef struct {
+    const void *g;
+    void *out;
+    const float *coefficients;
+    uint32_t steps;          /* 1 .. CO3_MAX_NS_STEPS                                          */
+    float eps;               /* >= 0                                                           */
+    uint64_t *status;        /* device [CO3_STATUS_WORDS] counters (added to)                  */
+    void *workspace;         /* device, co3_matrix_plan_workspace_bytes(), 256-byte aligned    */
+    size_t workspace_bytes;
+} co3_orthogonalize_args;
+int co3_orthogonalize(const co3_matrix_plan *plan, const co3_orthogonalize_args *args, void *stream);
+
+/* PS side, for the matrices of the model: the update that Muon makes of an average gradient (what
+ * co3_ps_aggregate writes), in place of w -= eta * average:
+ *   m = beta m + g;   u = g + beta m (nesterov) or m;   w = w (1 - eta weight_decay) - eta scale NS(u)
+ * NS as in co3_orthogonalize.  Elements outside the matrices stay as they are.  g may not be m or w.        */
+typedef struct {
+    const float *g;          /* device: the vector                                             */
+    float *momentum;         /* device: m, updated in place                                    */
+    float *model;            /* device: w, updated in place                                    */
+    const float *coefficients;
+    uint32_t steps;
+    float eps;
+    float eta, beta, weight_decay;
+    int32_t nesterov;
+    uint64_t *status;
+    void *workspace;
+    size_t workspace_bytes;
+} co3_muon_args;
+int co3_muon_update(const co3_matrix_plan *plan, const co3_muon_args *args, void *stream);
+
+/* Layer norm over rows of `cols` elements:  mean, var (of the row, biased), rstd = 1 / sqrt(var + eps),
+ * y = (x - mean) rstd weight + bias.  weight and bias (fp32 [cols], a layer's part of the flat model) may each
+ * be NULL (1 and 0), mean and rstd (fp32 [rows], for the backward pass) too.  Rows and y's rows lie x_stride and
+ * y_stride elements apart (>= cols).  All pointers are aligned as their elements are; y may be x.             */
+typedef struct {
+    const void *x;
+    void *y;
+    const float *weight, *bias;
+    float *mean, *rstd;
+    uint64_t rows;           /* 0 .. 2^31 - 1                                                  */
+    uint64_t x_stride, y_stride;
+    uint32_t cols;           /* 1 .. CO3_MAX_NORM_COLS                                         */
+    int32_t type;
+    float eps;
+    int32_t reserved;
+} co3_layernorm_args;
+#define CO3_MAX_NORM_COLS 32768u
+int co3_layernorm(const co3_layernorm_args *args, void *stream);
+
+/* Its backward pass for U users of rows_per_user rows each (rows u rows_per_user .. belong to user u):
+ *   t = dy weight,  xh = (x - mean) rstd,  dx = rstd (t - mean(t) - xh mean(t xh));
+ *   dweight[u] = sum over the user's rows of dy xh,  dbias[u] = sum of dy, in a fixed order.
+ * dweight and dbias (fp32; each may be NULL) lie grad_stride elements apart from user to user: they may be a
+ * layer's part of the users' gradients that co3_encode reads.  accumulate != 0 adds to what is there.  Users
+ * without rows have gradients of zero.  dx may be dy or x.
+ * workspace: device, co3_layernorm_backward_workspace_bytes(), 16-byte aligned; NULL where that is 0 or neither
+ * gradient is asked for.                                                                                     */
+typedef struct {
+    const void *dy, *x;
+    void *dx;
+    const float *weight;
+    const float *mean, *rstd;
+    float *dweight, *dbias;
+    uint64_t grad_stride;    /* >= cols where U > 1                                            */
+    uint64_t rows_per_user;  /* U rows_per_user <= 2^31 - 1                                    */
+    uint64_t dy_stride, x_stride, dx_stride;
+    uint32_t U;              /* 1 .. 65535                                                     */
+    uint32_t cols;
+    int32_t type;
+    int32_t accumulate;
+    void *workspace;
+    size_t workspace_bytes;
+} co3_layernorm_backward_args;
+size_t co3_layernorm_backward_workspace_bytes(uint32_t U, uint64_t rows_per_user, uint32_t cols);
+int co3_layernorm_backward(const co3_layernorm_backward_args *args, void *stream);
+
 /* ---- measurement aid ---------------------------------------------------------------------
  * Between co3_profile_begin() and co3_profile_end() every kernel the library launches is
  * bracketed by two HIP events recorded on the stream it is launched on.  co3_profile_end

@@ -29,6 +29,8 @@ EXPORTS = [
     "co3_model_weights_device", "co3_model_bias_device", "co3_plan_set_bias_device", "co3_bias_from_model", "co3_scale_from_model",
     "co3_plan_scale_workspace_bytes", "co3_model_scale_device", "co3_plan_set_gain_device",
     "co3_plan_bias_workspace_bytes", "co3_set_lookback_polls", "co3_encode_static", "co3_plan_set_gain",
+    "co3_matrix_plan_create", "co3_matrix_plan_destroy", "co3_matrix_plan_workspace_bytes", "co3_matrix_plan_elements",
+    "co3_orthogonalize", "co3_muon_update", "co3_layernorm", "co3_layernorm_backward_workspace_bytes", "co3_layernorm_backward",
 ]
 
 
@@ -63,6 +65,36 @@ class AggregateArgs(C.Structure):
     _fields_ = [("words", C.c_void_p), ("words_stride", C.c_uint64), ("chunk_offset", C.c_void_p),
                 ("sub_bits", C.c_void_p), ("books", C.c_void_p), ("out", C.c_void_p), ("status", C.c_void_p),
                 ("model", C.c_void_p), ("eta", C.c_float), ("reserved", C.c_int32)]
+
+
+class Matrix(C.Structure):
+    _fields_ = [("offset", C.c_uint64), ("ld", C.c_uint64), ("rows", C.c_uint32), ("cols", C.c_uint32), ("scale", C.c_float),
+                ("reserved", C.c_int32)]
+
+
+class OrthogonalizeArgs(C.Structure):
+    _fields_ = [("g", C.c_void_p), ("out", C.c_void_p), ("coefficients", C.c_void_p), ("steps", C.c_uint32), ("eps", C.c_float),
+                ("status", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
+class MuonArgs(C.Structure):
+    _fields_ = [("g", C.c_void_p), ("momentum", C.c_void_p), ("model", C.c_void_p), ("coefficients", C.c_void_p),
+                ("steps", C.c_uint32), ("eps", C.c_float), ("eta", C.c_float), ("beta", C.c_float), ("weight_decay", C.c_float),
+                ("nesterov", C.c_int32), ("status", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
+class LayernormArgs(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("y", C.c_void_p), ("weight", C.c_void_p), ("bias", C.c_void_p), ("mean", C.c_void_p),
+                ("rstd", C.c_void_p), ("rows", C.c_uint64), ("x_stride", C.c_uint64), ("y_stride", C.c_uint64),
+                ("cols", C.c_uint32), ("type", C.c_int32), ("eps", C.c_float), ("reserved", C.c_int32)]
+
+
+class LayernormBackwardArgs(C.Structure):
+    _fields_ = [("dy", C.c_void_p), ("x", C.c_void_p), ("dx", C.c_void_p), ("weight", C.c_void_p), ("mean", C.c_void_p),
+                ("rstd", C.c_void_p), ("dweight", C.c_void_p), ("dbias", C.c_void_p), ("grad_stride", C.c_uint64),
+                ("rows_per_user", C.c_uint64), ("dy_stride", C.c_uint64), ("x_stride", C.c_uint64), ("dx_stride", C.c_uint64),
+                ("U", C.c_uint32), ("cols", C.c_uint32), ("type", C.c_int32), ("accumulate", C.c_int32),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
 
 
 class KernelTime(C.Structure):
@@ -129,6 +161,19 @@ def lib():
                                            C.POINTER(C.c_float), C.POINTER(C.c_float), C.POINTER(C.c_double)]
         L.co3_set_lookback_polls.argtypes = [C.c_uint32]
         L.co3_set_lookback_polls.restype = None
+        L.co3_matrix_plan_create.argtypes = [C.c_uint32, C.c_void_p, C.c_int32, C.c_int32, C.POINTER(C.c_void_p)]
+        L.co3_matrix_plan_destroy.argtypes = [C.c_void_p]
+        L.co3_matrix_plan_destroy.restype = None
+        L.co3_matrix_plan_workspace_bytes.argtypes = [C.c_void_p]
+        L.co3_matrix_plan_workspace_bytes.restype = C.c_size_t
+        L.co3_matrix_plan_elements.argtypes = [C.c_void_p]
+        L.co3_matrix_plan_elements.restype = C.c_uint64
+        L.co3_orthogonalize.argtypes = [C.c_void_p, C.POINTER(OrthogonalizeArgs), C.c_void_p]
+        L.co3_muon_update.argtypes = [C.c_void_p, C.POINTER(MuonArgs), C.c_void_p]
+        L.co3_layernorm.argtypes = [C.POINTER(LayernormArgs), C.c_void_p]
+        L.co3_layernorm_backward_workspace_bytes.argtypes = [C.c_uint32, C.c_uint64, C.c_uint32]
+        L.co3_layernorm_backward_workspace_bytes.restype = C.c_size_t
+        L.co3_layernorm_backward.argtypes = [C.POINTER(LayernormBackwardArgs), C.c_void_p]
         L.co3_status_string.argtypes = [C.c_int]
         L.co3_status_string.restype = C.c_char_p
         _lib = L
@@ -141,9 +186,9 @@ def profile_begin():
 
 def profile_end():
     """{kernel name: (total ms, launches)} for the launches since profile_begin()."""
-    arr = (KernelTime * 16)()
+    arr = (KernelTime * 32)()
     n = C.c_uint32(0)
-    _check("co3_profile_end", lib().co3_profile_end(arr, 16, C.byref(n)))
+    _check("co3_profile_end", lib().co3_profile_end(arr, 32, C.byref(n)))
     return {arr[i].name.decode(): (arr[i].total_ms, int(arr[i].launches)) for i in range(n.value)}
 
 
@@ -444,3 +489,179 @@ def co3_ps_aggregate(plan, books, buf, out, stream=None, model=None, eta=0.0):
                       books.handle, None if out is None else out.data_ptr(), buf.status.data_ptr(),
                       None if model is None else model.data_ptr(), float(np.float32(eta)), 0)
     _check("co3_ps_aggregate", lib().co3_ps_aggregate(plan.handle, C.byref(a), _stream(stream)))
+
+
+# ---- training around the codec: layer norm, the orthogonalised update ----
+
+F32, BF16, F16 = 0, 1, 2
+PRODUCTS_PAIR, PRODUCTS_HIGH = 0, 1
+MAX_NS_STEPS = 32
+MAX_NORM_COLS = 32768
+MUON_COEFFICIENTS = (3.4445, -4.7750, 2.0315)
+
+
+def tensor_type(dtype):
+    """CO3_F32, CO3_BF16 or CO3_F16 of a torch dtype."""
+    import torch
+    types = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+    if dtype not in types:
+        raise TypeError(f"float32, bfloat16 or float16 tensors are taken, not {dtype}")
+    return types[dtype]
+
+
+class MatrixPlan:
+    """co3_matrix_plan: matrices (offset, rows, cols[, ld]) of a flat vector of `dtype`, and the factor of each one's
+    orthogonalised form (scales; None: 1).  products None: PRODUCTS_PAIR for float32, PRODUCTS_HIGH for 16-bit types."""
+
+    def __init__(self, matrices, dtype=None, scales=None, products=None):
+        import torch
+        dtype = torch.float32 if dtype is None else dtype
+        self.dtype, self.count = dtype, len(matrices)
+        self.products = (PRODUCTS_PAIR if dtype == torch.float32 else PRODUCTS_HIGH) if products is None else int(products)
+        scales = [1.0] * self.count if scales is None else [float(x) for x in scales]
+        assert len(scales) == self.count
+        table = (Matrix * self.count)()
+        for k, (m, scale) in enumerate(zip(matrices, scales)):
+            offset, rows, cols = (int(x) for x in m[:3])
+            table[k] = Matrix(offset, int(m[3]) if len(m) > 3 else cols, rows, cols, scale, 0)
+        h = C.c_void_p()
+        _check("co3_matrix_plan_create", lib().co3_matrix_plan_create(self.count, C.cast(table, C.c_void_p), tensor_type(dtype),
+                                                                      self.products, C.byref(h)))
+        self.handle = h
+        self.workspace_bytes = int(lib().co3_matrix_plan_workspace_bytes(h))
+        self.elements = int(lib().co3_matrix_plan_elements(h))
+
+    def close(self):
+        if getattr(self, "handle", None):
+            lib().co3_matrix_plan_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def _ns_coefficients(coefficients, steps):
+    """float32 [steps][3]: one triple for all steps, or one of each."""
+    c = np.asarray(coefficients, dtype=np.float32)
+    return np.ascontiguousarray(np.broadcast_to(c, (int(steps), 3)))
+
+
+def _matrix_vector(plan, t, name):
+    if t.dtype != plan.dtype or t.dim() != 1 or not t.is_contiguous() or t.numel() < plan.elements:
+        raise ValueError(f"{name}: a contiguous vector of at least {plan.elements} {plan.dtype} elements is taken")
+
+
+def _matrix_workspace(plan, workspace, device):
+    import torch
+    return torch.empty(plan.workspace_bytes, dtype=torch.uint8, device=device) if workspace is None else workspace
+
+
+def co3_orthogonalize(plan, g, out=None, steps=5, coefficients=MUON_COEFFICIENTS, eps=1e-7, workspace=None, status=None,
+                      stream=None):
+    """out = scale * Newton-Schulz iterate of every matrix of the flat vector g (out may be g; None: a new vector, with
+    zeros outside the matrices).  coefficients: (a, b, c) of every step, or `steps` triples.  status (int64
+    [STATUS_WORDS], or None): matrices whose norm is not finite are added to status[STAT_NONFINITE]."""
+    import torch
+    if out is None:
+        out = torch.zeros_like(g)
+    _matrix_vector(plan, g, "g")
+    _matrix_vector(plan, out, "out")
+    workspace = _matrix_workspace(plan, workspace, g.device)
+    c = _ns_coefficients(coefficients, steps)
+    a = OrthogonalizeArgs(g.data_ptr(), out.data_ptr(), c.ctypes.data, int(steps), float(eps),
+                          None if status is None else status.data_ptr(), workspace.data_ptr(), workspace.numel())
+    _check("co3_orthogonalize", lib().co3_orthogonalize(plan.handle, C.byref(a), _stream(stream)))
+    return out
+
+
+def co3_muon_update(plan, g, momentum, model, eta, beta=0.95, nesterov=True, weight_decay=0.0, steps=5,
+                    coefficients=MUON_COEFFICIENTS, eps=1e-7, workspace=None, status=None, stream=None):
+    """momentum = beta momentum + g, u = g + beta momentum (nesterov) or momentum, model = model (1 - eta weight_decay) -
+    eta scale NS(u), for every matrix of the float32 vectors; the elements outside the matrices stay."""
+    for t, name in ((g, "g"), (momentum, "momentum"), (model, "model")):
+        _matrix_vector(plan, t, name)
+    workspace = _matrix_workspace(plan, workspace, g.device)
+    c = _ns_coefficients(coefficients, steps)
+    a = MuonArgs(g.data_ptr(), momentum.data_ptr(), model.data_ptr(), c.ctypes.data, int(steps), float(eps), float(eta), float(beta),
+                 float(weight_decay), int(bool(nesterov)), None if status is None else status.data_ptr(), workspace.data_ptr(),
+                 workspace.numel())
+    _check("co3_muon_update", lib().co3_muon_update(plan.handle, C.byref(a), _stream(stream)))
+
+
+def _norm_rows(t, name):
+    """(users, rows per user, columns, elements between rows) of a [rows, cols] or [users, rows, cols] tensor."""
+    if t.dim() not in (2, 3) or (t.stride(-1) != 1 and t.shape[-1] > 1):
+        raise ValueError(f"{name}: [rows, cols] or [users, rows, cols] with contiguous rows is taken")
+    users, rows, cols = (1, *t.shape) if t.dim() == 2 else t.shape
+    stride = t.stride(-2) if rows > 1 else t.stride(0) if t.dim() == 3 and users > 1 else cols
+    if t.dim() == 3 and users > 1 and rows > 1 and t.stride(0) != rows * stride:
+        raise ValueError(f"{name}: all rows have to lie the same distance apart")
+    return users, rows, cols, stride
+
+
+def _norm_vector(t, n, name):
+    import torch
+    if t is not None and (t.dtype != torch.float32 or not t.is_contiguous() or t.numel() != n):
+        raise ValueError(f"{name}: {n} contiguous float32 elements are taken")
+    return None if t is None else t.data_ptr()
+
+
+def _like_rows(t, x, name):
+    if t.shape != x.shape or t.dtype != x.dtype:
+        raise ValueError(f"{name}: the shape and type of x are taken")
+
+
+def co3_layernorm(x, weight=None, bias=None, eps=1e-5, y=None, mean=None, rstd=None, stream=None):
+    """(y, mean, rstd) of x [rows, cols] or [users, rows, cols] (float32, bfloat16, float16; rows may lie apart): y of x's
+    type, mean and rstd float32 without the last dimension.  weight, bias: float32 [cols] or None.  y may be x."""
+    import torch
+    users, rows, cols, stride = _norm_rows(x, "x")
+    y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if y is None else y
+    mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if mean is None else mean
+    rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if rstd is None else rstd
+    _like_rows(y, x, "y")
+    a = LayernormArgs(x.data_ptr(), y.data_ptr(), _norm_vector(weight, cols, "weight"), _norm_vector(bias, cols, "bias"),
+                      _norm_vector(mean, users * rows, "mean"), _norm_vector(rstd, users * rows, "rstd"), users * rows, stride,
+                      _norm_rows(y, "y")[3], cols, tensor_type(x.dtype), float(eps), 0)
+    _check("co3_layernorm", lib().co3_layernorm(C.byref(a), _stream(stream)))
+    return y, mean, rstd
+
+
+def co3_layernorm_backward_workspace_bytes(users, rows, cols):
+    return int(lib().co3_layernorm_backward_workspace_bytes(int(users), int(rows), int(cols)))
+
+
+def _grad_rows(t, users, cols, name):
+    """Elements between two users' gradients."""
+    import torch
+    if t.dtype != torch.float32 or t.dim() not in (1, 2) or t.shape[-1] != cols or (t.stride(-1) != 1 and cols > 1) or \
+            (t.shape[0] if t.dim() == 2 else 1) != users:
+        raise ValueError(f"{name}: float32 [users, cols] with contiguous rows is taken ([cols] for one user)")
+    return t.stride(0) if t.dim() == 2 and users > 1 else cols
+
+
+def co3_layernorm_backward(dy, x, weight, mean, rstd, dx=None, dweight=None, dbias=None, accumulate=False, workspace=None,
+                           stream=None):
+    """dx of co3_layernorm, and where dweight / dbias are given (float32 [users, cols], rows may lie apart: a layer's part of
+    the users' gradients that co3_encode reads) the weight's gradients of every user: written, or added with accumulate."""
+    import torch
+    users, rows, cols, x_stride = _norm_rows(x, "x")
+    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if dx is None else dx
+    _like_rows(dy, x, "dy")
+    _like_rows(dx, x, "dx")
+    strides = [_grad_rows(t, users, cols, name) for t, name in ((dweight, "dweight"), (dbias, "dbias")) if t is not None]
+    if len(set(strides)) > 1:
+        raise ValueError("dweight and dbias: the same distance between users is taken")
+    if workspace is None and strides:
+        workspace = torch.empty(co3_layernorm_backward_workspace_bytes(users, rows, cols), dtype=torch.uint8, device=x.device)
+    a = LayernormBackwardArgs(dy.data_ptr(), x.data_ptr(), dx.data_ptr(), _norm_vector(weight, cols, "weight"),
+                              _norm_vector(mean, users * rows, "mean"), _norm_vector(rstd, users * rows, "rstd"),
+                              None if dweight is None else dweight.data_ptr(), None if dbias is None else dbias.data_ptr(),
+                              strides[0] if strides else 0, rows, _norm_rows(dy, "dy")[3], x_stride, _norm_rows(dx, "dx")[3], users,
+                              cols, tensor_type(x.dtype), int(bool(accumulate)), None if workspace is None else workspace.data_ptr(),
+                              0 if workspace is None else workspace.numel())
+    _check("co3_layernorm_backward", lib().co3_layernorm_backward(C.byref(a), _stream(stream)))
+    return dx

@@ -170,7 +170,8 @@ namespace co3 {
 
 // Per-kernel event timing (profile.cpp).  A ProfScope around a launch records two events on
 // the stream when profiling is on, and does nothing otherwise.
-enum KernelId { K_ZERO = 0, K_QUANTIZE, K_REDUCE_HIST, K_BUILD_BOOKS, K_CHUNK_BITS, K_SCAN, K_PACK, K_DECODE, K_AGGREGATE, K_FUSED, K_MOMENTS, K_FIT, K_MODEL_WEIGHTS, K_MODEL_BIAS, K_COUNT };
+enum KernelId { K_ZERO = 0, K_QUANTIZE, K_REDUCE_HIST, K_BUILD_BOOKS, K_CHUNK_BITS, K_SCAN, K_PACK, K_DECODE, K_AGGREGATE, K_FUSED, K_MOMENTS, K_FIT, K_MODEL_WEIGHTS, K_MODEL_BIAS,
+                K_ORTHO_NORM, K_ORTHO_PACK, K_ORTHO_GRAM, K_ORTHO_SQUARE, K_ORTHO_PRODUCT, K_LAYERNORM, K_LAYERNORM_BACKWARD, K_LAYERNORM_GRAD, K_COUNT };
 bool profile_enabled();
 class ProfScope {
 public:
@@ -238,5 +239,9 @@ hipError_t launch_build_books_wide(BookWide *books, uint32_t nbooks, uint32_t A,
 hipError_t launch_decode_wide(const Layout &lay, const co3_decode_args &a, const BookWide *books, hipStream_t s);
 hipError_t launch_aggregate_wide(const Layout &lay, const co3_aggregate_args &a, const BookWide *books,
                                  hipStream_t s);
+// layer norm (k_layernorm.hip)
+hipError_t launch_layernorm(const co3_layernorm_args &a, hipStream_t s);
+size_t layernorm_backward_workspace_bytes(uint32_t U, uint64_t rows_per_user, uint32_t cols);
+hipError_t launch_layernorm_backward(const co3_layernorm_backward_args &a, hipStream_t s);
 
 }  // namespace co3

@@ -1,0 +1,288 @@
+// Host side of the training operators declared in include/co3.h: argument checks, the plan of a set of matrices.
+#include <algorithm>
+#include <cmath>
+#include <new>
+#include <vector>
+
+#include "co3_internal.h"
+#include "ortho.h"
+#include "tensor_types.h"
+
+using namespace co3;
+
+namespace {
+
+struct DeviceGuard {
+    int prev = 0;
+    bool switched = false;
+    explicit DeviceGuard(int dev)
+    {
+        if (hipGetDevice(&prev) == hipSuccess && prev != dev) switched = hipSetDevice(dev) == hipSuccess;
+    }
+    ~DeviceGuard()
+    {
+        if (switched) (void)hipSetDevice(prev);
+    }
+};
+
+inline bool aligned(const void *p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+inline uint32_t up(uint32_t x, uint32_t n) { return (x + n - 1) / n * n; }
+inline size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
+inline bool valid_type(int32_t t) { return t == CO3_F32 || t == CO3_BF16 || t == CO3_F16; }
+
+constexpr uint32_t kMaxMatrices = 65536, kMaxSide = 1u << 20;
+constexpr uint64_t kMaxTiles = (1ull << 31) - 1;
+
+inline uint64_t end_of(const co3_matrix &m) { return m.offset + (uint64_t)(m.rows - 1) * m.ld + m.cols; }
+
+// Whether two matrices, a from b's first element or earlier on, share no element for certain: one ends before the other begins, or
+// their rows lie side by side at the same distance.
+bool apart(const co3_matrix &a, const co3_matrix &b)
+{
+    if (end_of(a) <= b.offset) return true;
+    if (a.ld != b.ld) return false;
+    const uint64_t col = (b.offset - a.offset) % a.ld;   // b's first column in a's rows
+    return col >= a.cols && col + b.cols <= a.ld;
+}
+
+int check_matrices(uint32_t count, const co3_matrix *m)
+{
+    for (uint32_t k = 0; k < count; ++k) {
+        if (m[k].rows == 0 || m[k].cols == 0 || m[k].rows > kMaxSide || m[k].cols > kMaxSide || m[k].ld < m[k].cols || !std::isfinite(m[k].scale))
+            return CO3_ERR_ARG;
+        if (m[k].ld > (1ull << 40) || m[k].offset > (1ull << 60)) return CO3_ERR_ARG;   // the last element's index fits 64 bits
+    }
+    std::vector<uint32_t> order(count), open;
+    for (uint32_t k = 0; k < count; ++k) order[k] = k;
+    std::sort(order.begin(), order.end(), [&](uint32_t a, uint32_t b) { return m[a].offset < m[b].offset; });
+    for (uint32_t k : order) {
+        open.erase(std::remove_if(open.begin(), open.end(), [&](uint32_t o) { return end_of(m[o]) <= m[k].offset; }), open.end());
+        for (uint32_t o : open)
+            if (!apart(m[o], m[k])) return CO3_ERR_ARG;
+        open.push_back(k);
+    }
+    return CO3_OK;
+}
+
+// The largest s p(s) = a s + b s^3 + c s^5 for s in [0, top], and the largest |b s^2 + c s^4|; the least of the former has to be
+// above -top too, since a singular value's sign is its vector's.  Both are smooth: 4096 points are near enough for limits of this use.
+bool stays_bounded(uint32_t steps, const float *coef)
+{
+    double top = 1.0;
+    for (uint32_t k = 0; k < steps; ++k) {
+        const double a = coef[3 * k], b = coef[3 * k + 1], c = coef[3 * k + 2];
+        if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) return false;
+        double most = 0.0, factor = 0.0;
+        for (int i = 0; i <= 4096; ++i) {
+            const double s = top * i / 4096.0, s2 = s * s;
+            most = std::max(most, std::fabs(s * (a + s2 * (b + s2 * c))));
+            factor = std::max(factor, std::fabs(s2 * (b + s2 * c)));
+        }
+        if (!(most <= 2.0) || !(factor <= 7.0)) return false;
+        top = most;
+    }
+    return true;
+}
+
+int build_plan(uint32_t count, const co3_matrix *matrices, co3_matrix_plan *p)
+{
+    OrthoLayout &l = p->lay;
+    const uint32_t PL = l.products == CO3_PRODUCTS_PAIR ? 2 : 1;
+    std::vector<MatDev> mats(count);
+    std::vector<PartDev> parts;
+    std::vector<TileDev> pack, gram, product;
+    uint64_t halves = 0;
+    for (uint32_t k = 0; k < count; ++k) {
+        const co3_matrix &c = matrices[k];
+        MatDev &m = mats[k];
+        m = {};
+        m.offset = c.offset; m.ld = c.ld; m.rows = c.rows; m.cols = c.cols; m.scale = c.scale;
+        m.tall = c.rows > c.cols ? 1u : 0u;
+        m.M = std::min(c.rows, c.cols);
+        m.N = std::max(c.rows, c.cols);
+        m.Mp = up(m.M, kTile);
+        m.Np = up(m.N, kTile);
+        const uint64_t plane_x = (uint64_t)m.Mp * m.Np, plane_a = (uint64_t)m.Mp * m.Mp;
+        m.x = halves; halves += 2 * plane_x;
+        m.xt = halves; halves += 2 * PL * plane_x;
+        m.a = halves; halves += PL * plane_a;
+        m.b = halves; halves += PL * plane_a;
+        p->elements = std::max(p->elements, end_of(c));
+        // parts of about 16384 elements, but at most 512 of a matrix: every workgroup that lays X out adds them up
+        const uint64_t n = (uint64_t)c.rows * c.cols, want = std::max<uint64_t>(16384, (n + 511) / 512 + 7 & ~7ull);
+        const bool whole = c.ld == c.cols;
+        const uint64_t lines = whole ? 1 : c.rows, len = whole ? n : c.cols;
+        const uint64_t cut = (len + want - 1) / want, piece = ((len + cut - 1) / cut + 7) & ~7ull, group = std::max<uint64_t>(1, want / len);
+        m.part = (uint32_t)parts.size();
+        for (uint64_t r = 0; r < lines; r += group)
+            for (uint64_t at = 0; at < len; at += piece)
+                parts.push_back({k, (uint32_t)std::min(group, lines - r), r * c.ld + at, std::min(piece, len - at)});
+        m.nparts = (uint32_t)parts.size() - m.part;
+        if (parts.size() > kMaxTiles) return CO3_ERR_CAPACITY;
+        for (uint32_t i = 0; i < m.Mp / kPackTile; ++i)
+            for (uint32_t j = 0; j < m.Np / kPackTile; ++j) pack.push_back({k, (uint16_t)i, (uint16_t)j});
+        for (uint32_t i = 0; i < m.Mp / kTile; ++i)
+            for (uint32_t j = 0; j <= i; ++j) gram.push_back({k, (uint16_t)i, (uint16_t)j});
+        for (uint32_t i = 0; i < m.Mp / kTile; ++i)
+            for (uint32_t j = 0; j < m.Np / kTile; ++j) product.push_back({k, (uint16_t)i, (uint16_t)j});
+        if (pack.size() > kMaxTiles) return CO3_ERR_CAPACITY;
+    }
+    l.nmat = count;
+    l.nparts = (uint32_t)parts.size();
+    l.npack = (uint32_t)pack.size();
+    l.ngram = (uint32_t)gram.size();
+    l.nproduct = (uint32_t)product.size();
+    l.halves = halves;
+    p->workspace_bytes = up256(parts.size() * sizeof(double)) + halves * sizeof(_Float16);
+
+    const size_t at_parts = up256(mats.size() * sizeof(MatDev)), at_pack = at_parts + up256(parts.size() * sizeof(PartDev));
+    const size_t at_gram = at_pack + up256(pack.size() * sizeof(TileDev)), at_product = at_gram + up256(gram.size() * sizeof(TileDev));
+    const size_t bytes = at_product + up256(product.size() * sizeof(TileDev));
+    if (hipMalloc(&p->tables, bytes) != hipSuccess) return CO3_ERR_HIP;
+    unsigned char *d = static_cast<unsigned char *>(p->tables);
+    const auto copy = [&](size_t at, const auto &v) {
+        return hipMemcpy(d + at, v.data(), v.size() * sizeof(v[0]), hipMemcpyHostToDevice) == hipSuccess;
+    };
+    if (!copy(0, mats) || !copy(at_parts, parts) || !copy(at_pack, pack) || !copy(at_gram, gram) || !copy(at_product, product))
+        return CO3_ERR_HIP;
+    l.mats = reinterpret_cast<const MatDev *>(d);
+    l.parts = reinterpret_cast<const PartDev *>(d + at_parts);
+    l.pack = reinterpret_cast<const TileDev *>(d + at_pack);
+    l.gram = reinterpret_cast<const TileDev *>(d + at_gram);
+    l.product = reinterpret_cast<const TileDev *>(d + at_product);
+    return CO3_OK;
+}
+
+// What both calls check, and the parts of the call that they share.
+int check_call(const co3_matrix_plan *plan, uint32_t steps, const float *coefficients, float eps, void *workspace, size_t workspace_bytes,
+               uint64_t *status, OrthoCall *c)
+{
+    if (!coefficients || steps == 0 || steps > CO3_MAX_NS_STEPS || !(eps >= 0.f) || std::isinf(eps) || !stays_bounded(steps, coefficients))
+        return CO3_ERR_ARG;
+    if (!workspace || !aligned(workspace, 256) || !aligned(status, 8)) return CO3_ERR_ARG;
+    if (workspace_bytes < plan->workspace_bytes) return CO3_ERR_CAPACITY;
+    c->steps = steps;
+    c->coefficients = coefficients;
+    c->eps = eps;
+    c->status = status;
+    c->partial = static_cast<double *>(workspace);
+    c->planes = reinterpret_cast<_Float16 *>(static_cast<unsigned char *>(workspace) + up256(plan->lay.nparts * sizeof(double)));
+    return CO3_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int co3_matrix_plan_create(uint32_t count, const co3_matrix *matrices, int32_t type, int32_t products, co3_matrix_plan **out)
+{
+    if (!out) return CO3_ERR_ARG;
+    *out = nullptr;
+    if (!matrices || count == 0 || count > kMaxMatrices || !valid_type(type) ||
+        (products != CO3_PRODUCTS_PAIR && products != CO3_PRODUCTS_HIGH))
+        return CO3_ERR_ARG;
+    co3_matrix_plan *p = nullptr;
+    int rc;
+    try {
+        rc = check_matrices(count, matrices);
+        if (rc != CO3_OK) return rc;
+        p = new co3_matrix_plan;
+        p->lay.type = type;
+        p->lay.products = products;
+        rc = hipGetDevice(&p->device) == hipSuccess ? build_plan(count, matrices, p) : CO3_ERR_HIP;
+    } catch (const std::exception &) {
+        rc = CO3_ERR_CAPACITY;
+    }
+    if (rc != CO3_OK) {
+        co3_matrix_plan_destroy(p);
+        return rc;
+    }
+    *out = p;
+    return CO3_OK;
+}
+
+void co3_matrix_plan_destroy(co3_matrix_plan *plan)
+{
+    if (!plan) return;
+    DeviceGuard guard(plan->device);
+    if (plan->tables) (void)hipFree(plan->tables);
+    delete plan;
+}
+
+size_t co3_matrix_plan_workspace_bytes(const co3_matrix_plan *plan) { return plan ? plan->workspace_bytes : 0; }
+uint64_t co3_matrix_plan_elements(const co3_matrix_plan *plan) { return plan ? plan->elements : 0; }
+
+int co3_orthogonalize(const co3_matrix_plan *plan, const co3_orthogonalize_args *a, void *stream)
+{
+    if (!plan || !a || !a->g || !a->out) return CO3_ERR_ARG;
+    const size_t size = type_bytes(plan->lay.type);
+    if (!aligned(a->g, size) || !aligned(a->out, size)) return CO3_ERR_ARG;
+    OrthoCall c = {};
+    if (int rc = check_call(plan, a->steps, a->coefficients, a->eps, a->workspace, a->workspace_bytes, a->status, &c); rc != CO3_OK) return rc;
+    c.g = a->g;
+    c.out = a->out;
+    DeviceGuard guard(plan->device);
+    return launch_orthogonalize(plan->lay, c, static_cast<hipStream_t>(stream)) == hipSuccess ? CO3_OK : CO3_ERR_HIP;
+}
+
+int co3_muon_update(const co3_matrix_plan *plan, const co3_muon_args *a, void *stream)
+{
+    if (!plan || !a || !a->g || !a->momentum || !a->model || plan->lay.type != CO3_F32) return CO3_ERR_ARG;
+    if (!aligned(a->g, 4) || !aligned(a->momentum, 4) || !aligned(a->model, 4)) return CO3_ERR_ARG;
+    if (a->g == a->momentum || a->g == a->model || a->momentum == a->model) return CO3_ERR_ARG;
+    if (!std::isfinite(a->eta) || !std::isfinite(a->beta) || !std::isfinite(a->weight_decay)) return CO3_ERR_ARG;
+    OrthoCall c = {};
+    if (int rc = check_call(plan, a->steps, a->coefficients, a->eps, a->workspace, a->workspace_bytes, a->status, &c); rc != CO3_OK) return rc;
+    c.g = a->g;
+    c.momentum = a->momentum;
+    c.model = a->model;
+    c.eta = a->eta;
+    c.beta = a->beta;
+    c.decay = a->weight_decay;
+    c.nesterov = a->nesterov;
+    DeviceGuard guard(plan->device);
+    return launch_orthogonalize(plan->lay, c, static_cast<hipStream_t>(stream)) == hipSuccess ? CO3_OK : CO3_ERR_HIP;
+}
+
+int co3_layernorm(const co3_layernorm_args *a, void *stream)
+{
+    if (!a || !valid_type(a->type) || a->cols == 0 || a->cols > CO3_MAX_NORM_COLS || a->rows >= (1ull << 31)) return CO3_ERR_ARG;
+    if (!(a->eps >= 0.f) || std::isinf(a->eps)) return CO3_ERR_ARG;
+    if (a->rows == 0) return CO3_OK;
+    const size_t size = type_bytes(a->type);
+    if (!a->x || !a->y || !aligned(a->x, size) || !aligned(a->y, size)) return CO3_ERR_ARG;
+    if (!aligned(a->weight, 4) || !aligned(a->bias, 4) || !aligned(a->mean, 4) || !aligned(a->rstd, 4)) return CO3_ERR_ARG;
+    if (a->x_stride < a->cols || a->y_stride < a->cols || (a->x == a->y && a->x_stride != a->y_stride)) return CO3_ERR_ARG;
+    return launch_layernorm(*a, static_cast<hipStream_t>(stream)) == hipSuccess ? CO3_OK : CO3_ERR_HIP;
+}
+
+size_t co3_layernorm_backward_workspace_bytes(uint32_t U, uint64_t rows_per_user, uint32_t cols)
+{
+    return U == 0 || U > 65535u || cols > CO3_MAX_NORM_COLS ? 0 : layernorm_backward_workspace_bytes(U, rows_per_user, cols);
+}
+
+int co3_layernorm_backward(const co3_layernorm_backward_args *a, void *stream)
+{
+    if (!a || !valid_type(a->type) || a->cols == 0 || a->cols > CO3_MAX_NORM_COLS || a->U == 0 || a->U > 65535u) return CO3_ERR_ARG;
+    if (a->rows_per_user >= (1ull << 31) || a->U * a->rows_per_user >= (1ull << 31)) return CO3_ERR_ARG;
+    const size_t size = type_bytes(a->type);
+    const bool grads = a->dweight || a->dbias;
+    if (!aligned(a->weight, 4) || !aligned(a->mean, 4) || !aligned(a->rstd, 4) || !aligned(a->dweight, 4) || !aligned(a->dbias, 4)) return CO3_ERR_ARG;
+    if (grads && a->U > 1 && a->grad_stride < a->cols) return CO3_ERR_ARG;
+    if (a->rows_per_user) {
+        if (!a->dy || !a->x || !a->dx || !a->mean || !a->rstd) return CO3_ERR_ARG;
+        if (!aligned(a->dy, size) || !aligned(a->x, size) || !aligned(a->dx, size)) return CO3_ERR_ARG;
+        if (a->dy_stride < a->cols || a->x_stride < a->cols || a->dx_stride < a->cols) return CO3_ERR_ARG;
+        if ((a->dx == a->dy && a->dx_stride != a->dy_stride) || (a->dx == a->x && a->dx_stride != a->x_stride)) return CO3_ERR_ARG;
+    } else if (!grads) {
+        return CO3_OK;
+    }
+    const size_t need = grads ? layernorm_backward_workspace_bytes(a->U, a->rows_per_user, a->cols) : 0;
+    if (need) {
+        if (!a->workspace || !aligned(a->workspace, 16)) return CO3_ERR_ARG;
+        if (a->workspace_bytes < need) return CO3_ERR_CAPACITY;
+    }
+    return launch_layernorm_backward(*a, static_cast<hipStream_t>(stream)) == hipSuccess ? CO3_OK : CO3_ERR_HIP;
+}
+
+}  // extern "C"

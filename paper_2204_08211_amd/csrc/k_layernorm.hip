@@ -1,0 +1,294 @@
+// Layer norm: forward pass, backward pass, the reduction of the weight's gradients per user.
+//
+// Forward:   mean, var of a row, rstd = 1 / sqrt(var + eps), y = (x - mean) rstd weight + bias
+// Backward:  t = dy weight, xh = (x - mean) rstd, dx = rstd (t - mean(t) - xh mean(t xh)),
+//            dweight[u] = sum over the rows of user u of dy xh, dbias[u] = sum of dy
+// Both are bound by memory: every element is read once and written once, the row stays in registers in between.  All
+// sums are fp32 over a lane's elements and then over the lanes in a fixed order; the variance is the mean of the squared
+// distances from the mean, which a mean far larger than the spread does not harm.
+#include "co3_internal.h"
+#include "tensor_types.h"
+
+namespace co3 {
+
+// TPR threads share a row: TPR <= 64 lanes of a wavefront, or the whole workgroup.  A thread holds CH packs of 16 bytes,
+// the packs of neighbouring threads next to each other.
+template <int TPR>
+__device__ inline float row_sum(float v, float *lds)
+{
+#pragma unroll
+    for (int o = (TPR < 64 ? TPR : 64) / 2; o; o >>= 1) v += __shfl_xor(v, o);
+    if (TPR > 64) {
+        const int w = threadIdx.x >> 6;
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) lds[w] = v;
+        __syncthreads();
+        v = lds[0];
+#pragma unroll
+        for (int i = 1; i < TPR / 64; ++i) v += lds[i];
+    }
+    return v;
+}
+
+template <typename T, int TPR, int CH>
+__global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_layernorm(co3_layernorm_args a)
+{
+    constexpr int V = kVec<T>, WG = TPR > 256 ? TPR : 256;
+    __shared__ float lds[WG / 64];
+    const uint64_t row = (uint64_t)blockIdx.x * (WG / TPR) + threadIdx.x / TPR;
+    const bool live = row < a.rows;   // a workgroup of several rows: the lanes of a row that is not there go along
+    const uint64_t r = live ? row : a.rows - 1;
+    const int at = (int)(threadIdx.x % TPR) * V, cols = (int)a.cols;
+    const T *x = static_cast<const T *>(a.x) + r * a.x_stride;
+    float v[CH][V];
+    float s = 0.f;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int j = at + c * TPR * V;
+        const auto p = load_pack<T, V>(x + j, cols - j);
+#pragma unroll
+        for (int i = 0; i < V; ++i) { v[c][i] = (float)p[i]; s += v[c][i]; }
+    }
+    const float n = 1.0f / (float)cols;
+    const float mean = row_sum<TPR>(s, lds) * n;
+    s = 0.f;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int j = at + c * TPR * V;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            v[c][i] = v[c][i] - mean;
+            s += j + i < cols ? v[c][i] * v[c][i] : 0.f;
+        }
+    }
+    const float rstd = 1.0f / sqrtf(row_sum<TPR>(s, lds) * n + a.eps);
+    if (!live) return;
+    if (threadIdx.x % TPR == 0) {
+        if (a.mean) a.mean[row] = mean;
+        if (a.rstd) a.rstd[row] = rstd;
+    }
+    T *y = static_cast<T *>(a.y) + row * a.y_stride;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int j = at + c * TPR * V;
+        if (j >= cols) break;
+        typename Pack<float, V>::V w, b;
+#pragma unroll
+        for (int i = 0; i < V; ++i) { w[i] = 1.f; b[i] = 0.f; }
+        if (a.weight) w = load_pack<float, V>(a.weight + j, cols - j);
+        if (a.bias) b = load_pack<float, V>(a.bias + j, cols - j);
+        typename Pack<T, V>::V p;
+#pragma unroll
+        for (int i = 0; i < V; ++i) p[i] = (T)(v[c][i] * rstd * w[i] + b[i]);
+        store_pack<T, V>(y + j, cols - j, p);
+    }
+}
+
+// Slices that a user's rows are cut into, one workgroup each.  A slice leaves a row of partial sums for either gradient, 16
+// bytes a column written and read again, so it has at least 32 rows of three tensors.
+constexpr uint32_t kSliceRows = 32, kSlices = 1024;
+static uint32_t backward_slices(uint32_t U, uint64_t rows)
+{
+    const uint64_t most = kSlices / U > 1 ? kSlices / U : 1;
+    const uint64_t n = (rows + kSliceRows - 1) / kSliceRows;
+    return (uint32_t)(n < 1 ? 1 : n < most ? n : most);
+}
+
+template <typename T, int TPR, int CH>
+__global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_layernorm_backward(co3_layernorm_backward_args a, uint32_t slices, float *partial)
+{
+    constexpr int V = kVec<T>, WG = TPR > 256 ? TPR : 256, ROWS = WG / TPR;
+    __shared__ float lds[2][WG / 64];
+    extern __shared__ float sums[];   // [2][cols], where several rows are on their way at a time
+    const uint32_t u = blockIdx.y;
+    const int sub = threadIdx.x / TPR, at = (int)(threadIdx.x % TPR) * V, cols = (int)a.cols;
+    const uint64_t base = (uint64_t)u * a.rows_per_user;
+    const uint64_t r0 = a.rows_per_user * blockIdx.x / slices, r1 = a.rows_per_user * (blockIdx.x + 1) / slices;
+    const float n = 1.0f / (float)cols;
+    float dw[CH][V], db[CH][V];
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int i = 0; i < V; ++i) dw[c][i] = db[c][i] = 0.f;
+    for (uint64_t k = r0; k < r1; k += ROWS) {   // the same number of turns for all threads
+        const bool live = k + sub < r1;
+        const uint64_t r = base + (live ? k + sub : k);
+        const T *x = static_cast<const T *>(a.x) + r * a.x_stride, *dy = static_cast<const T *>(a.dy) + r * a.dy_stride;
+        typename Pack<T, V>::V px[CH], pd[CH];
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int j = at + c * TPR * V;
+            px[c] = load_pack<T, V>(x + j, cols - j);
+            pd[c] = load_pack<T, V>(dy + j, live ? cols - j : 0);   // a row that is not there adds nothing
+        }
+        const float mean = a.mean[r], rstd = a.rstd[r];
+        float xh[CH][V], t[CH][V], s1 = 0.f, s2 = 0.f;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int j = at + c * TPR * V;
+            typename Pack<float, V>::V w;
+#pragma unroll
+            for (int i = 0; i < V; ++i) w[i] = 1.f;
+            if (a.weight) w = load_pack<float, V>(a.weight + j, cols - j);
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const float d = (float)pd[c][i];
+                const bool in = live && j + i < cols;
+                xh[c][i] = in ? ((float)px[c][i] - mean) * rstd : 0.f;
+                t[c][i] = d * w[i];
+                s1 += t[c][i];
+                s2 += t[c][i] * xh[c][i];
+                dw[c][i] += d * xh[c][i];
+                db[c][i] += d;
+            }
+        }
+        s1 = row_sum<TPR>(s1, lds[0]) * n;
+        s2 = row_sum<TPR>(s2, lds[1]) * n;
+        if (!live) continue;
+        T *dx = static_cast<T *>(a.dx) + r * a.dx_stride;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int j = at + c * TPR * V;
+            if (j >= cols) break;
+            typename Pack<T, V>::V p;
+#pragma unroll
+            for (int i = 0; i < V; ++i) p[i] = (T)(rstd * (t[c][i] - s1 - xh[c][i] * s2));
+            store_pack<T, V>(dx + j, cols - j, p);
+        }
+    }
+    if (!a.dweight && !a.dbias) return;
+    if (ROWS > 1) {   // the workgroup's rows after one another
+        for (int w = 0; w < ROWS; ++w) {
+            if (sub == w) {
+#pragma unroll
+                for (int c = 0; c < CH; ++c)
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        const int j = at + c * TPR * V + i;
+                        if (j >= cols) continue;
+                        sums[j] = dw[c][i] = (w ? sums[j] : 0.f) + dw[c][i];
+                        sums[cols + j] = db[c][i] = (w ? sums[cols + j] : 0.f) + db[c][i];
+                    }
+            }
+            __syncthreads();
+        }
+        if (sub != ROWS - 1) return;
+    }
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const int j = at + c * TPR * V + i;
+            if (j >= cols) continue;
+            if (slices > 1) {
+                float *p = partial + ((uint64_t)u * slices + blockIdx.x) * 2 * cols;
+                p[j] = dw[c][i];
+                p[cols + j] = db[c][i];
+            } else {
+                if (a.dweight) { float *p = a.dweight + u * a.grad_stride + j; *p = a.accumulate ? *p + dw[c][i] : dw[c][i]; }
+                if (a.dbias) { float *p = a.dbias + u * a.grad_stride + j; *p = a.accumulate ? *p + db[c][i] : db[c][i]; }
+            }
+        }
+}
+
+// The slices' sums of a user, 64 columns of either gradient a workgroup.
+__global__ __launch_bounds__(256) void k_layernorm_grad(co3_layernorm_backward_args a, uint32_t slices, const float *partial)
+{
+    __shared__ float part[4][64];
+    const uint32_t u = blockIdx.y, lane = threadIdx.x & 63u, w = threadIdx.x >> 6;
+    const uint64_t c = (uint64_t)blockIdx.x * 64 + lane, cols = a.cols;   // dweight's columns, then dbias's
+    float s = 0.f;
+    if (c < 2 * cols)
+        for (uint32_t p = w; p < slices; p += 4) s += partial[((uint64_t)u * slices + p) * 2 * cols + c];
+    part[w][lane] = s;
+    __syncthreads();
+    if (w || c >= 2 * cols) return;
+    s = part[0][lane] + part[1][lane] + part[2][lane] + part[3][lane];
+    float *out = c < cols ? a.dweight : a.dbias;
+    if (!out) return;
+    out += u * a.grad_stride + (c < cols ? c : c - cols);
+    *out = a.accumulate ? *out + s : s;
+}
+
+template <typename T, int TPR, int CH>
+static void forward(const co3_layernorm_args &a, hipStream_t s)
+{
+    constexpr int WG = TPR > 256 ? TPR : 256, ROWS = WG / TPR;
+    k_layernorm<T, TPR, CH><<<dim3((uint32_t)((a.rows + ROWS - 1) / ROWS)), dim3(WG), 0, s>>>(a);
+}
+
+template <typename T, int TPR, int CH>
+static void backward(const co3_layernorm_backward_args &a, uint32_t slices, float *partial, hipStream_t s)
+{
+    constexpr int WG = TPR > 256 ? TPR : 256;
+    k_layernorm_backward<T, TPR, CH><<<dim3(slices, a.U), dim3(WG), WG > TPR ? 8 * a.cols : 0, s>>>(a, slices, partial);
+}
+
+template <typename T>
+static void forward_of(const co3_layernorm_args &a, hipStream_t s)
+{
+    const uint32_t packs = (a.cols + kVec<T> - 1) / kVec<T>;
+    if (packs <= 8) forward<T, 8, 1>(a, s);
+    else if (packs <= 16) forward<T, 16, 1>(a, s);
+    else if (packs <= 32) forward<T, 32, 1>(a, s);
+    else if (packs <= 64) forward<T, 64, 1>(a, s);
+    else if (packs <= 128) forward<T, 64, 2>(a, s);
+    else if (packs <= 256) forward<T, 64, 4>(a, s);
+    else if (packs <= 512) forward<T, 64, 8>(a, s);
+    else if (packs <= 1024) forward<T, 256, 4>(a, s);
+    else if (packs <= 2048) forward<T, 256, 8>(a, s);
+    else if (packs <= 4096) forward<T, 1024, 4>(a, s);
+    else forward<T, 1024, 8>(a, s);
+}
+
+template <typename T>
+static void backward_of(const co3_layernorm_backward_args &a, uint32_t slices, float *partial, hipStream_t s)
+{
+    const uint32_t packs = (a.cols + kVec<T> - 1) / kVec<T>;
+    if (packs <= 8) backward<T, 8, 1>(a, slices, partial, s);
+    else if (packs <= 16) backward<T, 16, 1>(a, slices, partial, s);
+    else if (packs <= 32) backward<T, 32, 1>(a, slices, partial, s);
+    else if (packs <= 64) backward<T, 64, 1>(a, slices, partial, s);
+    else if (packs <= 128) backward<T, 64, 2>(a, slices, partial, s);
+    else if (packs <= 256) backward<T, 64, 4>(a, slices, partial, s);
+    else if (packs <= 512) backward<T, 256, 2>(a, slices, partial, s);
+    else if (packs <= 1024) backward<T, 256, 4>(a, slices, partial, s);
+    else if (packs <= 4096) backward<T, 1024, 4>(a, slices, partial, s);
+    else backward<T, 1024, 8>(a, slices, partial, s);
+}
+
+size_t layernorm_backward_workspace_bytes(uint32_t U, uint64_t rows_per_user, uint32_t cols)
+{
+    const uint32_t slices = backward_slices(U, rows_per_user);
+    return slices > 1 ? (size_t)U * slices * 2 * cols * sizeof(float) : 0;
+}
+
+hipError_t launch_layernorm(const co3_layernorm_args &a, hipStream_t s)
+{
+    ProfScope prof(K_LAYERNORM, s);
+    if (a.type == CO3_F32) forward_of<float>(a, s);
+    else if (a.type == CO3_BF16) forward_of<__bf16>(a, s);
+    else forward_of<_Float16>(a, s);
+    return hipGetLastError();
+}
+
+hipError_t launch_layernorm_backward(const co3_layernorm_backward_args &a, hipStream_t s)
+{
+    const bool grads = a.dweight || a.dbias;
+    const uint32_t slices = backward_slices(a.U, a.rows_per_user);
+    float *partial = static_cast<float *>(a.workspace);
+    {
+        ProfScope prof(K_LAYERNORM_BACKWARD, s);
+        if (a.type == CO3_F32) backward_of<float>(a, slices, partial, s);
+        else if (a.type == CO3_BF16) backward_of<__bf16>(a, slices, partial, s);
+        else backward_of<_Float16>(a, slices, partial, s);
+    }
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    if (grads && slices > 1) {
+        ProfScope prof(K_LAYERNORM_GRAD, s);
+        k_layernorm_grad<<<dim3((2 * a.cols + 63) / 64, a.U), dim3(256), 0, s>>>(a, slices, partial);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace co3

@@ -1,0 +1,70 @@
+// What the host side and the kernels of the Newton-Schulz iteration share (co3_train.cpp, k_ortho.hip).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "co3.h"
+
+namespace co3 {
+
+// The workspace holds every matrix as X (M x N, M <= N: the transpose of a tall one), padded by zeros to whole tiles, so that the
+// products have no edges.  Planes of fp16, in elements from the workspace's planes on; the low parts lie behind the high ones.
+struct MatDev {
+    uint64_t offset, ld;        // in the caller's vector
+    uint64_t x;                 // X, hi and lo: [Mp][Np]
+    uint64_t xt;                // X^T twice, of one step and of the next: [Np][Mp]; hi, or hi and lo
+    uint64_t a, b;              // A = X X^T and B = b A + c A A: [Mp][Mp]; hi, or hi and lo
+    uint32_t rows, cols;        // as the caller has it
+    uint32_t M, N, Mp, Np;
+    uint32_t part, nparts;      // its partial sums of squares
+    float scale;
+    uint32_t tall;              // X is the transpose
+};
+
+// One workgroup's tile of a launch over all matrices.
+struct TileDev {
+    uint32_t mat;
+    uint16_t i, j;
+};
+// One workgroup's part of a sum of squares: `lines` lines of `len` elements, from element `at` of the matrix on.
+struct PartDev {
+    uint32_t mat, lines;
+    uint64_t at, len;
+};
+
+constexpr uint32_t kPackTile = 64;     // elements either way of a tile of the kernel that lays X out
+constexpr uint32_t kTile = 128;        // of a tile of the products
+
+struct OrthoLayout {
+    const MatDev *mats;
+    const PartDev *parts;
+    const TileDev *pack, *gram, *product;     // tiles: of X; of A and B, the lower half; of X
+    uint32_t nmat, nparts, npack, ngram, nproduct;
+    int32_t type, products;
+    uint64_t halves;                          // fp16 elements of all planes
+};
+
+struct OrthoCall {
+    const void *g;
+    void *out;                 // nullptr: the model is updated
+    float *momentum, *model;
+    float eta, beta, decay, eps;
+    int32_t nesterov;
+    uint32_t steps;
+    const float *coefficients; // host
+    uint64_t *status;
+    double *partial;           // device [nparts]
+    _Float16 *planes;          // device
+};
+hipError_t launch_orthogonalize(const OrthoLayout &lay, const OrthoCall &c, hipStream_t s);
+
+}  // namespace co3
+
+struct co3_matrix_plan {
+    co3::OrthoLayout lay = {};
+    void *tables = nullptr;    // device: all of the layout's
+    uint64_t elements = 0;
+    size_t workspace_bytes = 0;
+    int device = 0;
+};
