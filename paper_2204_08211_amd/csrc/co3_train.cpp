@@ -1,7 +1,9 @@
 // Host side of the training operators declared in include/co3.h: argument checks, the plan of a set of matrices.
 #include <algorithm>
 #include <cmath>
+#include <functional>
 #include <new>
+#include <queue>
 #include <vector>
 
 #include "co3_internal.h"
@@ -84,6 +86,54 @@ bool stays_bounded(uint32_t steps, const float *coef)
     return true;
 }
 
+// Tiles of T x T of a product over all matrices, those with the longest sums first.  Workgroups go to the eight XCDs in turn, each with
+// a cache of its own, so every eighth tile is from a neighbourhood: rows of tiles, eight tiles high, are cut into eight pieces.
+std::vector<TileDev> tiles(const std::vector<MatDev> &mats, uint32_t T, bool lower)
+{
+    std::vector<uint32_t> order(mats.size());
+    for (uint32_t k = 0; k < order.size(); ++k) order[k] = k;
+    std::stable_sort(order.begin(), order.end(), [&](uint32_t a, uint32_t b) { return mats[a].Np > mats[b].Np; });
+    std::vector<TileDev> out;
+    for (uint32_t k : order) {
+        const uint32_t ni = (mats[k].Mp + T - 1) / T, nj = lower ? ni : (mats[k].Np + T - 1) / T;
+        std::vector<TileDev> own;
+        for (uint32_t i0 = 0; i0 < ni; i0 += 8)
+            for (uint32_t j = 0; j < nj; ++j)
+                for (uint32_t i = i0; i < std::min(i0 + 8, ni); ++i)
+                    if (!lower || j <= i) own.push_back({k, (uint16_t)i, (uint16_t)j});
+        const size_t n = own.size();
+        std::vector<size_t> start(9);
+        for (size_t x = 0; x <= 8; ++x) start[x] = (n / 8) * x + std::min<size_t>(x, n % 8);
+        for (size_t q = 0; q < n; ++q) out.push_back(own[start[q % 8] + q / 8]);
+    }
+    return out;
+}
+
+// Elements either way of the tiles of a product: those with which 256 workgroups at a time are done first, by the time that a workgroup
+// takes for its sums (measured: relative to 256 x 256, a CU multiplies at 0.7 of the rate with tiles of 128, at 0.35 with tiles of 64).
+uint32_t choose_tile(const std::vector<MatDev> &mats, bool lower, bool square, std::vector<TileDev> *out)
+{
+    uint32_t best = 0;
+    double least = 0.0;
+    for (uint32_t T : {256u, 128u, 64u}) {
+        const std::vector<TileDev> v = tiles(mats, T, lower);
+        const double rate = T == 256 ? 1.0 : T == 128 ? 0.7 : 0.35;
+        std::priority_queue<double, std::vector<double>, std::greater<double>> busy;
+        double last = 0.0;
+        for (const TileDev &t : v) {
+            const MatDev &m = mats[t.mat];
+            const double K = lower ? (double)m.Np + (square ? m.Mp : 0.0) : (double)m.Mp;
+            double at = (K + 256.0) * T * T / rate;   // the ends of a tile take about as long as 256 more products
+            if (busy.size() >= 256) { at += busy.top(); busy.pop(); }
+            busy.push(at);
+            last = std::max(last, at);
+        }
+        if (!best || last < least) { best = T; least = last; *out = v; }
+        if (v.size() > 65536) break;   // large enough to fill the chip either way
+    }
+    return best;
+}
+
 int build_plan(uint32_t count, const co3_matrix *matrices, co3_matrix_plan *p)
 {
     OrthoLayout &l = p->lay;
@@ -91,7 +141,7 @@ int build_plan(uint32_t count, const co3_matrix *matrices, co3_matrix_plan *p)
     std::vector<MatDev> mats(count);
     std::vector<PartDev> parts;
     std::vector<TileDev> pack, gram, product;
-    uint64_t halves = 0;
+    uint64_t halves = 0, diagonals = 0;
     for (uint32_t k = 0; k < count; ++k) {
         const co3_matrix &c = matrices[k];
         MatDev &m = mats[k];
@@ -100,8 +150,9 @@ int build_plan(uint32_t count, const co3_matrix *matrices, co3_matrix_plan *p)
         m.tall = c.rows > c.cols ? 1u : 0u;
         m.M = std::min(c.rows, c.cols);
         m.N = std::max(c.rows, c.cols);
-        m.Mp = up(m.M, kTile);
-        m.Np = up(m.N, kTile);
+        m.Mp = up(m.M, kBlock);
+        m.Np = up(m.N, kBlock);
+        m.diag = diagonals; diagonals += 2 * m.Mp;
         const uint64_t plane_x = (uint64_t)m.Mp * m.Np, plane_a = (uint64_t)m.Mp * m.Mp;
         m.x = halves; halves += 2 * plane_x;
         m.xt = halves; halves += 2 * PL * plane_x;
@@ -119,21 +170,19 @@ int build_plan(uint32_t count, const co3_matrix *matrices, co3_matrix_plan *p)
                 parts.push_back({k, (uint32_t)std::min(group, lines - r), r * c.ld + at, std::min(piece, len - at)});
         m.nparts = (uint32_t)parts.size() - m.part;
         if (parts.size() > kMaxTiles) return CO3_ERR_CAPACITY;
-        for (uint32_t i = 0; i < m.Mp / kPackTile; ++i)
-            for (uint32_t j = 0; j < m.Np / kPackTile; ++j) pack.push_back({k, (uint16_t)i, (uint16_t)j});
-        for (uint32_t i = 0; i < m.Mp / kTile; ++i)
-            for (uint32_t j = 0; j <= i; ++j) gram.push_back({k, (uint16_t)i, (uint16_t)j});
-        for (uint32_t i = 0; i < m.Mp / kTile; ++i)
-            for (uint32_t j = 0; j < m.Np / kTile; ++j) product.push_back({k, (uint16_t)i, (uint16_t)j});
+        for (uint32_t i = 0; i < m.Mp / kBlock; ++i)
+            for (uint32_t j = 0; j < m.Np / kBlock; ++j) pack.push_back({k, (uint16_t)i, (uint16_t)j});
         if (pack.size() > kMaxTiles) return CO3_ERR_CAPACITY;
     }
+    l.gram_tile = choose_tile(mats, true, true, &gram);
+    l.product_tile = choose_tile(mats, false, false, &product);
     l.nmat = count;
     l.nparts = (uint32_t)parts.size();
     l.npack = (uint32_t)pack.size();
     l.ngram = (uint32_t)gram.size();
     l.nproduct = (uint32_t)product.size();
-    l.halves = halves;
-    p->workspace_bytes = up256(parts.size() * sizeof(double)) + halves * sizeof(_Float16);
+    l.diagonals = diagonals;
+    p->workspace_bytes = up256(parts.size() * sizeof(double)) + up256(diagonals * sizeof(float)) + halves * sizeof(_Float16);
 
     const size_t at_parts = up256(mats.size() * sizeof(MatDev)), at_pack = at_parts + up256(parts.size() * sizeof(PartDev));
     const size_t at_gram = at_pack + up256(pack.size() * sizeof(TileDev)), at_product = at_gram + up256(gram.size() * sizeof(TileDev));
@@ -166,7 +215,9 @@ int check_call(const co3_matrix_plan *plan, uint32_t steps, const float *coeffic
     c->eps = eps;
     c->status = status;
     c->partial = static_cast<double *>(workspace);
-    c->planes = reinterpret_cast<_Float16 *>(static_cast<unsigned char *>(workspace) + up256(plan->lay.nparts * sizeof(double)));
+    unsigned char *at = static_cast<unsigned char *>(workspace) + up256(plan->lay.nparts * sizeof(double));
+    c->diagonals = reinterpret_cast<float *>(at);
+    c->planes = reinterpret_cast<_Float16 *>(at + up256(plan->lay.diagonals * sizeof(float)));
     return CO3_OK;
 }
 

@@ -13,6 +13,8 @@
 // while large ones stay: the rounding of the iterate to 11 bits, spread over all directions, grows with them (a
 // matrix of one dominant direction and 10^-3 noise: 9e-2 off, with the pair 2e-4).  Roundings of A and B need no pair for
 // results of 16 bits: where the singular values are small, so are A and B beside a (2e-3 off, the size of bf16's own rounding).
+#include <type_traits>
+
 #include "co3_internal.h"
 #include "ortho.h"
 #include "tensor_types.h"
@@ -86,7 +88,7 @@ template <typename T, bool MUON, bool PAIR>
 __global__ __launch_bounds__(256) void k_ortho_pack(OrthoLayout lay, OrthoCall c)
 {
     __shared__ double lds[4];
-    __shared__ float tile[kPackTile * kPitch];
+    __shared__ float tile[kBlock * kPitch];
     const TileDev t = lay.pack[blockIdx.x];
     const MatDev m = lay.mats[t.mat];
     double s = 0.0;
@@ -97,9 +99,9 @@ __global__ __launch_bounds__(256) void k_ortho_pack(OrthoLayout lay, OrthoCall c
     if (!finite && t.i == 0 && t.j == 0 && threadIdx.x == 0 && c.status)
         atomicAdd(reinterpret_cast<unsigned long long *>(c.status + CO3_STAT_NONFINITE), 1ull);
 
-    const uint32_t gr = (m.tall ? t.j : t.i) * kPackTile, gc = (m.tall ? t.i : t.j) * kPackTile;   // in the caller's matrix
+    const uint32_t gr = (m.tall ? t.j : t.i) * kBlock, gc = (m.tall ? t.i : t.j) * kBlock;   // in the caller's matrix
     const uint32_t lane = threadIdx.x & 63u;
-    for (uint32_t r = threadIdx.x >> 6; r < kPackTile; r += 4) {
+    for (uint32_t r = threadIdx.x >> 6; r < kBlock; r += 4) {
         float v = 0.f;
         if (gr + r < m.rows && gc + lane < m.cols) {
             const uint64_t at = m.offset + (uint64_t)(gr + r) * m.ld + gc + lane;
@@ -125,11 +127,11 @@ __global__ __launch_bounds__(256) void k_ortho_pack(OrthoLayout lay, OrthoCall c
             lo[i] = l;
         }
         if (across == (m.tall != 0)) {
-            const uint64_t at = (uint64_t)(t.i * kPackTile + r) * m.Np + t.j * kPackTile + k;
+            const uint64_t at = (uint64_t)(t.i * kBlock + r) * m.Np + t.j * kBlock + k;
             *reinterpret_cast<half8 *>(x + at) = hi;
             *reinterpret_cast<half8 *>(x + plane + at) = lo;
         } else {
-            const uint64_t at = (uint64_t)(t.j * kPackTile + r) * m.Mp + t.i * kPackTile + k;
+            const uint64_t at = (uint64_t)(t.j * kBlock + r) * m.Mp + t.i * kBlock + k;
             *reinterpret_cast<half8 *>(xt + at) = hi;
             if (PAIR) *reinterpret_cast<half8 *>(xt + plane + at) = lo;
         }
@@ -140,52 +142,99 @@ __global__ __launch_bounds__(256) void k_ortho_pack(OrthoLayout lay, OrthoCall c
 
 enum { GRAM, SQUARE, PRODUCT, LAST };
 
-// acc[i][j] += sum over k of P[i][k] Q[j][k] for a wavefront's 64 x 64 of a workgroup's 128 x 128, from rows of K elements.
-constexpr int kDepth = 32, kRow = kDepth + 8;   // elements of a row in LDS; 16 bytes apart from the next
+// The shape of a workgroup's tile: WI x WJ wavefronts of FI x FJ fragments of 32 x 32.
+template <int T> struct Shape;
+template <> struct Shape<256> { static constexpr int WI = 2, WJ = 4, FI = 4, FJ = 2; };
+template <> struct Shape<128> { static constexpr int WI = 2, WJ = 2, FI = 2, FJ = 2; };
+template <> struct Shape<64> { static constexpr int WI = 2, WJ = 2, FI = 1, FJ = 1; };
+template <int T> constexpr int kThreads = 64 * Shape<T>::WI * Shape<T>::WJ;
+// Elements of a row that are in LDS at a time: 128 bytes of it, or 64 of either part of a pair.
+template <bool PAIR> constexpr int kDepth = PAIR ? 32 : 64;
+template <int T> constexpr int kStage = 2 * T * 64;   // fp16 elements of P's and Q's rows of one turn
+
+// Where 16 bytes of a row lie in LDS: as they come, but exchanged within the row by its number, so that the same 16 bytes of sixteen
+// rows, which sixteen lanes read at a time, lie in different ones of the 64 banks.
 template <bool PAIR>
-__device__ inline void multiply(const _Float16 *p, const _Float16 *q, uint64_t plane_p, uint64_t plane_q, uint32_t K, _Float16 *lds,
-                                float16v (&acc)[2][2])
+__device__ inline int staged(int row, int chunk)
 {
-    constexpr int PL = PAIR ? 2 : 1, T = (int)kTile;
+    return PAIR ? row * 32 + (chunk ^ (row >> 2 & 3)) * 8 : row * 64 + (chunk ^ (row >> 1 & 7)) * 8;
+}
+
+// acc[i][j] += sum over k of P[i][k] Q[j][k] for a wavefront's part of the tile, from rows of K elements; rows past the last are
+// the last.  While the matrix instructions work on one turn's rows, the next turn's are on their way to registers, and go to the other
+// half of LDS afterwards.
+template <bool PAIR, int T>
+__device__ inline void multiply(const _Float16 *p, const _Float16 *q, uint32_t p_rows, uint32_t q_rows, uint64_t plane_p, uint64_t plane_q,
+                                uint32_t K, _Float16 *lds, float16v (&acc)[Shape<T>::FI][Shape<T>::FJ])
+{
+    constexpr int PL = PAIR ? 2 : 1, D = kDepth<PAIR>, CH = D / 8, WG = kThreads<T>, H = T * CH / WG;
+    constexpr int FI = Shape<T>::FI, FJ = Shape<T>::FJ;
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int wi = (w >> 1) * 64, wj = (w & 1) * 64;
-    const int row = threadIdx.x >> 2, part = (threadIdx.x & 3) * 8;
-    for (uint32_t k0 = 0; k0 < K; k0 += kDepth) {
-        half8 v[2 * PL][2];
+    const int wi = w / Shape<T>::WJ * FI * 32, wj = w % Shape<T>::WJ * FJ * 32;
+    const int row = threadIdx.x / CH, chunk = threadIdx.x % CH;
+    const _Float16 *from[2][H];
 #pragma unroll
-        for (int pl = 0; pl < 2 * PL; ++pl)
+    for (int h = 0; h < H; ++h) {
+        const uint32_t r = row + h * (WG / CH);
+        from[0][h] = p + (uint64_t)(r < p_rows ? r : p_rows - 1) * K + chunk * 8;
+        from[1][h] = q + (uint64_t)(r < q_rows ? r : q_rows - 1) * K + chunk * 8;
+    }
+    half8 v[2][PL][H];
+    const auto fetch = [&](uint32_t k0) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const _Float16 *src = pl < PL ? p + pl * plane_p : q + (pl - PL) * plane_q;
-                v[pl][h] = *reinterpret_cast<const half8 *>(src + (uint64_t)(row + h * 64) * K + k0 + part);
-            }
-        __syncthreads();
-#pragma unroll
-        for (int pl = 0; pl < 2 * PL; ++pl)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) *reinterpret_cast<half8 *>(lds + (pl * T + row + h * 64) * kRow + part) = v[pl][h];
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < kDepth; k += 16) {
-            half8 a[PL][2], b[PL][2];
+        for (int o = 0; o < 2; ++o)
 #pragma unroll
             for (int pl = 0; pl < PL; ++pl)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    a[pl][h] = *reinterpret_cast<const half8 *>(lds + (pl * T + wi + h * 32 + lane % 32) * kRow + k + lane / 32 * 8);
-                    b[pl][h] = *reinterpret_cast<const half8 *>(lds + ((PL + pl) * T + wj + h * 32 + lane % 32) * kRow + k + lane / 32 * 8);
-                }
+                for (int h = 0; h < H; ++h) v[o][pl][h] = *reinterpret_cast<const half8 *>(from[o][h] + pl * (o ? plane_q : plane_p) + k0);
+    };
+    const auto put = [&](_Float16 *to) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+        for (int o = 0; o < 2; ++o)
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    if (PAIR) {
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[0][i], b[PL - 1][j], acc[i][j], 0, 0, 0);
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[PL - 1][i], b[0][j], acc[i][j], 0, 0, 0);
-                    }
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[0][i], b[0][j], acc[i][j], 0, 0, 0);
-                }
+            for (int pl = 0; pl < PL; ++pl)
+#pragma unroll
+                for (int h = 0; h < H; ++h)
+                    *reinterpret_cast<half8 *>(to + (o * PL + pl) * T * D + staged<PAIR>(row + h * (WG / CH), chunk)) = v[o][pl][h];
+    };
+    fetch(0);
+    put(lds);
+    __syncthreads();
+    int at = 0;
+    for (uint32_t k0 = 0; k0 < K; k0 += D) {
+        const bool more = k0 + D < K;
+        if (more) fetch(k0 + D);
+        const _Float16 *s = lds + at;
+#pragma unroll
+        for (int k = 0; k < D / 8; k += 2) {
+            half8 a[PL][FI], b[PL][FJ];
+#pragma unroll
+            for (int pl = 0; pl < PL; ++pl) {
+#pragma unroll
+                for (int i = 0; i < FI; ++i)
+                    a[pl][i] = *reinterpret_cast<const half8 *>(s + pl * T * D + staged<PAIR>(wi + i * 32 + lane % 32, k + lane / 32));
+#pragma unroll
+                for (int j = 0; j < FJ; ++j)
+                    b[pl][j] = *reinterpret_cast<const half8 *>(s + (PL + pl) * T * D + staged<PAIR>(wj + j * 32 + lane % 32, k + lane / 32));
+            }
+            if (PAIR) {   // the small products first
+#pragma unroll
+                for (int i = 0; i < FI; ++i)
+#pragma unroll
+                    for (int j = 0; j < FJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[0][i], b[PL - 1][j], acc[i][j], 0, 0, 0);
+#pragma unroll
+                for (int i = 0; i < FI; ++i)
+#pragma unroll
+                    for (int j = 0; j < FJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[PL - 1][i], b[0][j], acc[i][j], 0, 0, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < FI; ++i)
+#pragma unroll
+                for (int j = 0; j < FJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[0][i], b[0][j], acc[i][j], 0, 0, 0);
         }
+        at ^= kStage<T>;
+        if (more) put(lds + at);
+        __syncthreads();
     }
 }
 
@@ -220,106 +269,141 @@ __device__ inline void store_result(const OrthoLayout &lay, const OrthoCall &c, 
     }
 }
 
+// One product of every matrix.  A and B are kept without their diagonals, which are fp32: most of a matrix near the identity is
+// there, and of its rounding.  With d for A's and e for B's diagonal:
+//   B_ij = b A_ij + c ((A A)_ij + (d_i + d_j) A_ij),  e_i = b d_i + c ((A A)_ii + d_i^2),  X <- a X + e hi(X) + B hi(X)
+// (the same X in both last terms: an error of X that B as a whole would take out stays taken out).
 // `turn`: which of the two transposes this step reads.
-template <int OP, bool PAIR>
-__global__ __launch_bounds__(256) void k_ortho_product(OrthoLayout lay, OrthoCall c, Polynomial f, uint32_t turn)
+template <int OP, bool PAIR, int T>
+__global__ __launch_bounds__(kThreads<T>, T == 128 ? 2 : 1) void k_ortho_product(OrthoLayout lay, OrthoCall c, Polynomial f, uint32_t turn)
 {
-    constexpr int PL = PAIR ? 2 : 1;
-    constexpr size_t kStage = sizeof(_Float16) * 2 * PL * kTile * kRow, kFold = sizeof(float) * 4 * 64 * kPitch;
-    __shared__ __attribute__((aligned(16))) unsigned char lds[kStage > kFold ? kStage : kFold];
+    constexpr int PL = PAIR ? 2 : 1, WG = kThreads<T>, FI = Shape<T>::FI, FJ = Shape<T>::FJ;
+    // The results go through LDS in blocks of 64 x 64: a wavefront's own, one after the other, or the workgroup's only one.
+    constexpr int kTeam = T == 64 ? WG : 64, kFolds = WG / kTeam, kBlocks = T == 256 ? 2 : 1;
+    constexpr size_t kBytes = sizeof(_Float16) * 2 * kStage<T>, kFold = sizeof(float) * kFolds * 64 * kPitch;
+    __shared__ __attribute__((aligned(16))) unsigned char lds[kBytes > kFold ? kBytes : kFold];
     const TileDev t = OP == GRAM || OP == SQUARE ? lay.gram[blockIdx.x] : lay.product[blockIdx.x];
     const MatDev &m = lay.mats[t.mat];
-    const uint32_t K = OP == GRAM ? m.Np : m.Mp;
+    const uint32_t K = OP == GRAM ? m.Np : m.Mp, cols = OP == PRODUCT || OP == LAST ? m.Np : m.Mp;
     const uint64_t plane_x = (uint64_t)m.Mp * m.Np, plane_a = (uint64_t)m.Mp * m.Mp;
     _Float16 *x = c.planes + m.x, *xt = c.planes + m.xt + turn * PL * plane_x, *xt_next = c.planes + m.xt + (turn ^ 1u) * PL * plane_x;
     _Float16 *a = c.planes + m.a, *b = c.planes + m.b;
+    float *diag_a = c.diagonals + m.diag, *diag_b = diag_a + m.Mp;
     const _Float16 *p = OP == GRAM ? x : OP == SQUARE ? a : b;
     const _Float16 *q = OP == GRAM ? x : OP == SQUARE ? a : xt;
 
-    float16v acc[2][2] = {};
-    multiply<PAIR>(p + (uint64_t)t.i * kTile * K, q + (uint64_t)t.j * kTile * K, OP == GRAM ? plane_x : plane_a,
-                   OP == SQUARE ? plane_a : plane_x, K, reinterpret_cast<_Float16 *>(lds), acc);
-    __syncthreads();
+    float16v acc[FI][FJ] = {};
+    multiply<PAIR, T>(p + (uint64_t)t.i * T * K, q + (uint64_t)t.j * T * K, m.Mp - t.i * T, cols - t.j * T, OP == GRAM ? plane_x : plane_a,
+                      OP == SQUARE ? plane_a : plane_x, K, reinterpret_cast<_Float16 *>(lds), acc);
 
-    // A wavefront's 64 x 64 through LDS: along its rows first, then along its columns.
-    const uint32_t lane = threadIdx.x & 63u, w = threadIdx.x >> 6;
-    float *fold = reinterpret_cast<float *>(lds) + w * 64 * kPitch;
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int e = 0; e < 16; ++e)
-                fold[(i * 32 + e / 4 * 8 + lane / 32 * 4 + e % 4) * kPitch + j * 32 + lane % 32] = acc[i][j][e];
-    __syncthreads();
-    const uint32_t i0 = t.i * kTile + (w >> 1) * 64, j0 = t.j * kTile + (w & 1) * 64;
+    const uint32_t lane = threadIdx.x & 63u, w = threadIdx.x >> 6, tid = threadIdx.x % kTeam;
+    const uint32_t wi = w / Shape<T>::WJ * FI * 32, wj = w % Shape<T>::WJ * FJ * 32;
+    float *fold = reinterpret_cast<float *>(lds) + threadIdx.x / kTeam * 64 * kPitch;
     const bool turned = OP == PRODUCT || (OP == LAST && m.tall) || ((OP == GRAM || OP == SQUARE) && t.i != t.j);
+    const auto finish = [&](auto which) __attribute__((always_inline)) {
+        constexpr int block = decltype(which)::value, BI = FI / kBlocks;
+        if (block) __syncthreads();
+        const uint32_t in_i = T == 64 ? wi : 0u, in_j = T == 64 ? wj : 0u;   // the wavefront's place in the block
 #pragma unroll
-    for (uint32_t pass = 0; pass < 8; ++pass) {
-        const uint32_t r = pass * 8 + lane / 8, k = lane % 8 * 8;
-        float *at = fold + r * kPitch + k;
-        const uint64_t to = (uint64_t)(i0 + r) * (OP == PRODUCT || OP == LAST ? m.Np : m.Mp) + j0 + k;
-        float v[8];
-        half8 hi, lo;
-        if (OP == SQUARE || OP == PRODUCT || OP == LAST) {
-            const _Float16 *old = OP == SQUARE ? a : x;
-            hi = *reinterpret_cast<const half8 *>(old + to);
-            lo = half8{};
-            if (PAIR || OP != SQUARE) lo = *reinterpret_cast<const half8 *>(old + (OP == SQUARE ? plane_a : plane_x) + to);
-        }
+        for (int i = 0; i < BI; ++i)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            if (OP == GRAM) v[e] = at[e] * (1.f / kScaleX);
-            if (OP == SQUARE) v[e] = ((float)hi[e] + (float)lo[e]) * (f.b * (kScaleB / kScaleX)) + at[e] * (f.c * (kScaleB / kScaleX / kScaleX));
-            if (OP == PRODUCT || OP == LAST) v[e] = f.a * ((float)hi[e] + (float)lo[e]) + at[e] * (1.f / kScaleB);
-        }
-        if (OP == LAST) {
-            if (!m.tall) store_result(lay, c, m, i0 + r, j0 + k, v);
-            else
+            for (int j = 0; j < FJ; ++j)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) at[e] = v[e];
-            continue;
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            _Float16 h, l;
-            split(v[e], h, l);
-            hi[e] = h;
-            lo[e] = l;
-            const uint32_t both = (uint32_t)__builtin_bit_cast(uint16_t, h) | (uint32_t)__builtin_bit_cast(uint16_t, l) << 16;
-            at[e] = __builtin_bit_cast(float, both);
-        }
-        _Float16 *dst = OP == GRAM ? a : OP == SQUARE ? b : x;
-        *reinterpret_cast<half8 *>(dst + to) = hi;
-        if (PAIR || OP == PRODUCT) *reinterpret_cast<half8 *>(dst + (OP == PRODUCT ? plane_x : plane_a) + to) = lo;
-    }
-    if (!turned) return;   // the same for the whole workgroup
-    __syncthreads();
-#pragma unroll
-    for (uint32_t pass = 0; pass < 8; ++pass) {
-        const uint32_t r = pass * 8 + lane / 8, k = lane % 8 * 8;   // column r of the tile, rows k ..
-        if (OP == LAST) {
+                for (int e = 0; e < 16; ++e)
+                    fold[(in_i + i * 32 + e / 4 * 8 + lane / 32 * 4 + e % 4) * kPitch + in_j + j * 32 + lane % 32] = acc[block * BI + i][j][e];
+        __syncthreads();
+        const uint32_t i0 = t.i * T + (T == 64 ? 0u : wi + block * 64), j0 = t.j * T + (T == 64 ? 0u : wj);
+        const bool there = i0 < m.Mp && j0 < cols;   // the same for all threads of the block
+#pragma unroll 2
+        for (uint32_t r = there ? tid / 8 : 64u; r < 64; r += kTeam / 8) {
+            const uint32_t k = tid % 8 * 8;
+            float *at = fold + r * kPitch + k;
+            const uint64_t to = (uint64_t)(i0 + r) * cols + j0 + k;
             float v[8];
+            half8 hi = {}, lo = {};
+            if (OP != GRAM) {
+                const _Float16 *old = OP == SQUARE ? a : x;
+                hi = *reinterpret_cast<const half8 *>(old + to);
+                if (PAIR || OP != SQUARE) lo = *reinterpret_cast<const half8 *>(old + (OP == SQUARE ? plane_a : plane_x) + to);
+            }
+            const float di = OP == GRAM ? 0.f : (OP == SQUARE ? diag_a : diag_b)[i0 + r] * (1.f / kScaleX);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = fold[(k + e) * kPitch + r];
-            store_result(lay, c, m, j0 + r, i0 + k, v);
-            continue;
-        }
-        half8 hi, lo;
+            for (int e = 0; e < 8; ++e) {
+                if (OP == GRAM) v[e] = at[e] * (1.f / kScaleX);
+                if (OP == SQUARE) {
+                    const bool on = i0 + r == j0 + k + e;
+                    const float d = diag_a[j0 + k + e], aij = on ? d : (float)hi[e] + (float)lo[e];
+                    v[e] = f.b * aij + f.c * (at[e] * (1.f / kScaleX) + (on ? di : di + d * (1.f / kScaleX)) * aij);
+                }
+                if (OP == PRODUCT || OP == LAST)
+                    v[e] = f.a * ((float)hi[e] + (float)lo[e]) + (di * (PAIR ? (float)hi[e] + (float)lo[e] : (float)hi[e]) + at[e] * (1.f / kScaleB));
+            }
+            if (OP == LAST) {
+                if (!m.tall) store_result(lay, c, m, i0 + r, j0 + k, v);
+                else
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const uint32_t both = __builtin_bit_cast(uint32_t, fold[(k + e) * kPitch + r]);
-            hi[e] = __builtin_bit_cast(_Float16, (uint16_t)both);
-            lo[e] = __builtin_bit_cast(_Float16, (uint16_t)(both >> 16));
+                    for (int e = 0; e < 8; ++e) at[e] = v[e];
+                continue;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                if (OP != PRODUCT && i0 + r == j0 + k + e) {
+                    (OP == GRAM ? diag_a : diag_b)[i0 + r] = v[e];
+                    v[e] = 0.f;
+                }
+                if (OP == SQUARE) v[e] *= kScaleB / kScaleX;
+                _Float16 h, l;
+                split(v[e], h, l);
+                hi[e] = h;
+                lo[e] = l;
+                const uint32_t both = (uint32_t)__builtin_bit_cast(uint16_t, h) | (uint32_t)__builtin_bit_cast(uint16_t, l) << 16;
+                at[e] = __builtin_bit_cast(float, both);
+            }
+            _Float16 *dst = OP == GRAM ? a : OP == SQUARE ? b : x;
+            *reinterpret_cast<half8 *>(dst + to) = hi;
+            if (PAIR || OP == PRODUCT) *reinterpret_cast<half8 *>(dst + (OP == PRODUCT ? plane_x : plane_a) + to) = lo;
         }
-        _Float16 *dst = OP == GRAM ? a : OP == SQUARE ? b : xt_next;
-        const uint64_t to = (uint64_t)(j0 + r) * m.Mp + i0 + k;
-        *reinterpret_cast<half8 *>(dst + to) = hi;
-        if (PAIR) *reinterpret_cast<half8 *>(dst + (OP == PRODUCT ? plane_x : plane_a) + to) = lo;
-    }
+        if (!turned) return;   // the same for the whole workgroup
+        __syncthreads();
+#pragma unroll 2
+        for (uint32_t r = there ? tid / 8 : 64u; r < 64; r += kTeam / 8) {   // column r of the block
+            const uint32_t k = tid % 8 * 8;
+            if (OP == LAST) {
+                float v[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = fold[(k + e) * kPitch + r];
+                store_result(lay, c, m, j0 + r, i0 + k, v);
+                continue;
+            }
+            half8 hi, lo;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t both = __builtin_bit_cast(uint32_t, fold[(k + e) * kPitch + r]);
+                hi[e] = __builtin_bit_cast(_Float16, (uint16_t)both);
+                lo[e] = __builtin_bit_cast(_Float16, (uint16_t)(both >> 16));
+            }
+            _Float16 *dst = OP == GRAM ? a : OP == SQUARE ? b : xt_next;
+            const uint64_t to = (uint64_t)(j0 + r) * m.Mp + i0 + k;
+            *reinterpret_cast<half8 *>(dst + to) = hi;
+            if (PAIR) *reinterpret_cast<half8 *>(dst + (OP == PRODUCT ? plane_x : plane_a) + to) = lo;
+        }
+    };
+    finish(std::integral_constant<int, 0>{});
+    if constexpr (kBlocks == 2) finish(std::integral_constant<int, 1>{});
 }
 
 // ---- the call -----------------------------------------------------------------------------------------------
+
+template <int OP, bool PAIR>
+static void product(const OrthoLayout &lay, const OrthoCall &c, const Polynomial &f, uint32_t turn, hipStream_t s)
+{
+    constexpr bool lower = OP == GRAM || OP == SQUARE;
+    const uint32_t tile = lower ? lay.gram_tile : lay.product_tile, n = lower ? lay.ngram : lay.nproduct;
+    ProfScope prof(OP == GRAM ? K_ORTHO_GRAM : OP == SQUARE ? K_ORTHO_SQUARE : K_ORTHO_PRODUCT, s);
+    if (tile == 256) k_ortho_product<OP, PAIR, 256><<<dim3(n), dim3(kThreads<256>), 0, s>>>(lay, c, f, turn);
+    else if (tile == 128) k_ortho_product<OP, PAIR, 128><<<dim3(n), dim3(kThreads<128>), 0, s>>>(lay, c, f, turn);
+    else k_ortho_product<OP, PAIR, 64><<<dim3(n), dim3(kThreads<64>), 0, s>>>(lay, c, f, turn);
+}
 
 template <typename T, bool MUON, bool PAIR>
 static hipError_t iterate(const OrthoLayout &lay, const OrthoCall &c, hipStream_t s)
@@ -334,17 +418,10 @@ static hipError_t iterate(const OrthoLayout &lay, const OrthoCall &c, hipStream_
     }
     for (uint32_t k = 0; k < c.steps; ++k) {
         const Polynomial f = {c.coefficients[3 * k], c.coefficients[3 * k + 1], c.coefficients[3 * k + 2]};
-        {
-            ProfScope prof(K_ORTHO_GRAM, s);
-            k_ortho_product<GRAM, PAIR><<<dim3(lay.ngram), dim3(256), 0, s>>>(lay, c, f, 0);
-        }
-        {
-            ProfScope prof(K_ORTHO_SQUARE, s);
-            k_ortho_product<SQUARE, PAIR><<<dim3(lay.ngram), dim3(256), 0, s>>>(lay, c, f, 0);
-        }
-        ProfScope prof(K_ORTHO_PRODUCT, s);
-        if (k + 1 < c.steps) k_ortho_product<PRODUCT, PAIR><<<dim3(lay.nproduct), dim3(256), 0, s>>>(lay, c, f, k & 1u);
-        else k_ortho_product<LAST, PAIR><<<dim3(lay.nproduct), dim3(256), 0, s>>>(lay, c, f, k & 1u);
+        product<GRAM, PAIR>(lay, c, f, 0, s);
+        product<SQUARE, PAIR>(lay, c, f, 0, s);
+        if (k + 1 < c.steps) product<PRODUCT, PAIR>(lay, c, f, k & 1u, s);
+        else product<LAST, PAIR>(lay, c, f, k & 1u, s);
     }
     return hipGetLastError();
 }

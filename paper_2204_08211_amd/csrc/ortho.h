@@ -8,8 +8,8 @@
 
 namespace co3 {
 
-// The workspace holds every matrix as X (M x N, M <= N: the transpose of a tall one), padded by zeros to whole tiles, so that the
-// products have no edges.  Planes of fp16, in elements from the workspace's planes on; the low parts lie behind the high ones.
+// The workspace holds every matrix as X (M x N, M <= N: the transpose of a tall one), padded by zeros to multiples of 64 either way, so
+// that the products have no edges.  Planes of fp16, in elements from the workspace's planes on; the low parts lie behind the high ones.
 struct MatDev {
     uint64_t offset, ld;        // in the caller's vector
     uint64_t x;                 // X, hi and lo: [Mp][Np]
@@ -18,6 +18,7 @@ struct MatDev {
     uint32_t rows, cols;        // as the caller has it
     uint32_t M, N, Mp, Np;
     uint32_t part, nparts;      // its partial sums of squares
+    uint64_t diag;              // the diagonals of A and of B, fp32 [2][Mp], from the workspace's diagonals on
     float scale;
     uint32_t tall;              // X is the transpose
 };
@@ -33,16 +34,16 @@ struct PartDev {
     uint64_t at, len;
 };
 
-constexpr uint32_t kPackTile = 64;     // elements either way of a tile of the kernel that lays X out
-constexpr uint32_t kTile = 128;        // of a tile of the products
+constexpr uint32_t kBlock = 64;        // what X is padded to, and a tile of the kernel that lays it out, either way
 
 struct OrthoLayout {
     const MatDev *mats;
     const PartDev *parts;
     const TileDev *pack, *gram, *product;     // tiles: of X; of A and B, the lower half; of X
     uint32_t nmat, nparts, npack, ngram, nproduct;
+    uint32_t gram_tile, product_tile;         // elements either way of a tile: 64, 128 or 256
     int32_t type, products;
-    uint64_t halves;                          // fp16 elements of all planes
+    uint64_t diagonals;                       // fp32 elements of all diagonals
 };
 
 struct OrthoCall {
@@ -55,6 +56,7 @@ struct OrthoCall {
     const float *coefficients; // host
     uint64_t *status;
     double *partial;           // device [nparts]
+    float *diagonals;          // device
     _Float16 *planes;          // device
 };
 hipError_t launch_orthogonalize(const OrthoLayout &lay, const OrthoCall &c, hipStream_t s);
