@@ -79,6 +79,14 @@ __device__ inline void split(float v, _Float16 &hi, _Float16 &lo)
     lo = (_Float16)(v - (float)hi);
 }
 
+// Where eight values from column k (a multiple of 8) of row r of a plane of K columns begin.  Pairs have 16 high and 16 low parts in
+// turn, so that 64 bytes of a row are what a turn of the products takes of it, in either form.
+template <bool PAIR>
+__device__ inline uint64_t place(uint32_t r, uint32_t k, uint32_t K)
+{
+    return PAIR ? (uint64_t)r * 2 * K + k / 16 * 32 + k % 16 : (uint64_t)r * K + k;
+}
+
 // What a tile of 64 x 64 floats in LDS is read and written by: 65 words a row, so that neither eight columns of eight rows nor
 // eight rows of eight columns meet in a bank.
 constexpr int kPitch = 65;
@@ -127,13 +135,13 @@ __global__ __launch_bounds__(256) void k_ortho_pack(OrthoLayout lay, OrthoCall c
             lo[i] = l;
         }
         if (across == (m.tall != 0)) {
-            const uint64_t at = (uint64_t)(t.i * kBlock + r) * m.Np + t.j * kBlock + k;
-            *reinterpret_cast<half8 *>(x + at) = hi;
-            *reinterpret_cast<half8 *>(x + plane + at) = lo;
+            _Float16 *to = x + place<PAIR>(t.i * kBlock + r, t.j * kBlock + k, m.Np);
+            *reinterpret_cast<half8 *>(to) = hi;
+            *reinterpret_cast<half8 *>(to + (PAIR ? 16 : plane)) = lo;
         } else {
-            const uint64_t at = (uint64_t)(t.j * kBlock + r) * m.Mp + t.i * kBlock + k;
-            *reinterpret_cast<half8 *>(xt + at) = hi;
-            if (PAIR) *reinterpret_cast<half8 *>(xt + plane + at) = lo;
+            _Float16 *to = xt + place<PAIR>(t.j * kBlock + r, t.i * kBlock + k, m.Mp);
+            *reinterpret_cast<half8 *>(to) = hi;
+            if (PAIR) *reinterpret_cast<half8 *>(to + 16) = lo;
         }
     }
 }
@@ -148,94 +156,141 @@ template <> struct Shape<256> { static constexpr int WI = 2, WJ = 4, FI = 4, FJ 
 template <> struct Shape<128> { static constexpr int WI = 2, WJ = 2, FI = 2, FJ = 2; };
 template <> struct Shape<64> { static constexpr int WI = 2, WJ = 2, FI = 1, FJ = 1; };
 template <int T> constexpr int kThreads = 64 * Shape<T>::WI * Shape<T>::WJ;
-// Elements of a row that are in LDS at a time: 128 bytes of it, or 64 of either part of a pair.
-template <bool PAIR> constexpr int kDepth = PAIR ? 32 : 64;
-template <int T> constexpr int kStage = 2 * T * 64;   // fp16 elements of P's and Q's rows of one turn
+// A turn takes 64 bytes of every row of P and of Q: 32 values, or 16 pairs.  LDS holds four turns.
+template <bool PAIR> constexpr int kDepth = PAIR ? 16 : 32;
+constexpr int kTurn = 32, kRing = 4;                  // fp16 numbers of a row in a turn; turns in LDS
+template <int T> constexpr int kStage = 2 * T * kTurn;   // fp16 numbers of a turn
 
-// Where 16 bytes of a row lie in LDS: as they come, but exchanged within the row by its number, so that the same 16 bytes of sixteen
-// rows, which sixteen lanes read at a time, lie in different ones of the 64 banks.
-template <bool PAIR>
-__device__ inline int staged(int row, int chunk)
+// Where 16 bytes of a row lie in its 64 bytes in LDS: exchanged by the row's number, so that the same 16 bytes of sixteen rows, which
+// sixteen lanes read at a time, lie in different ones of the 64 banks.
+__device__ inline int exchanged(int row, int chunk) { return chunk ^ (row >> 2 & 3); }
+
+// 64 lanes' 16 bytes from memory to LDS, without a register in between: from base + offset (of every lane) + k, to `lds` + 16 lane.
+// Written out, since the compiler would wait for all loads to LDS before every read of LDS.  Who reads waits with wait_loads().
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+__device__ inline void load_to_lds(u32x4 base, uint32_t offset, uint32_t k, uint32_t lds)
 {
-    return PAIR ? row * 32 + (chunk ^ (row >> 2 & 3)) * 8 : row * 64 + (chunk ^ (row >> 1 & 7)) * 8;
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" : : "s"(lds), "v"(offset), "s"(base), "s"(k) : "memory");
+}
+// Until all but the wavefront's last `left` loads are there.
+template <int left>
+__device__ inline void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" : : "n"(left) : "memory"); }
+
+// All wavefronts of the workgroup, each with what it asked of LDS.  (__syncthreads() would wait for the loads to LDS as well.)
+__device__ inline void meet()
+{
+    asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" : : : "memory");
 }
 
-// acc[i][j] += sum over k of P[i][k] Q[j][k] for a wavefront's part of the tile, from rows of K elements; rows past the last are
-// the last.  While the matrix instructions work on one turn's rows, the next turn's are on their way to registers, and go to the other
-// half of LDS afterwards.
-template <bool PAIR, int T>
-__device__ inline void multiply(const _Float16 *p, const _Float16 *q, uint32_t p_rows, uint32_t q_rows, uint64_t plane_p, uint64_t plane_q,
-                                uint32_t K, _Float16 *lds, float16v (&acc)[Shape<T>::FI][Shape<T>::FJ])
+// A buffer of `bytes` from p on, for load_to_lds.
+__device__ inline u32x4 buffer_of(const void *p, uint32_t bytes)
 {
-    constexpr int PL = PAIR ? 2 : 1, D = kDepth<PAIR>, CH = D / 8, WG = kThreads<T>, H = T * CH / WG;
-    constexpr int FI = Shape<T>::FI, FJ = Shape<T>::FJ;
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const uint64_t at = reinterpret_cast<uint64_t>(p);
+    u32x4 r = {(uint32_t)at, (uint32_t)(at >> 32) & 0xffffu, bytes, 0x00027000u};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = (uint32_t)__builtin_amdgcn_readfirstlane((int)r[i]);
+    return r;
+}
+
+// acc[i][j] += sum over k of P[i][k] Q[j][k] for a wavefront's part of the tile, from rows of K values; rows past the last are
+// the last.  Three turns are on their way to LDS while one is multiplied.  With eight wavefronts, two on a SIMD, four read
+// a turn's rows from LDS while the other four multiply, and the other way round: a wait ahead of them keeps the second half a
+// phase behind.
+template <bool PAIR, int T>
+__device__ __forceinline__ void multiply(const _Float16 *p, const _Float16 *q, uint32_t p_rows, uint32_t q_rows, uint32_t K, _Float16 *lds,
+                                         float16v (&acc)[Shape<T>::FI][Shape<T>::FJ])
+{
+    constexpr int FI = Shape<T>::FI, FJ = Shape<T>::FJ, W = Shape<T>::WI * Shape<T>::WJ;
+    constexpr int LOADS = 2 * T / 16 / W;   // of 16 rows each, of a wavefront in a turn
+    constexpr bool kPhases = W == 8;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wi = w / Shape<T>::WJ * FI * 32, wj = w % Shape<T>::WJ * FJ * 32;
-    const int row = threadIdx.x / CH, chunk = threadIdx.x % CH;
-    const _Float16 *from[2][H];
+    const uint32_t row_bytes = K * (PAIR ? 4u : 2u), turns = K / kDepth<PAIR>;
+    const u32x4 base_p = buffer_of(p, (p_rows < T ? p_rows : T) * row_bytes), base_q = buffer_of(q, (q_rows < T ? q_rows : T) * row_bytes);
+    const uint32_t lds0 = (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) _Float16 *)lds);
+    uint32_t offset[LOADS], to[LOADS];
 #pragma unroll
-    for (int h = 0; h < H; ++h) {
-        const uint32_t r = row + h * (WG / CH);
-        from[0][h] = p + (uint64_t)(r < p_rows ? r : p_rows - 1) * K + chunk * 8;
-        from[1][h] = q + (uint64_t)(r < q_rows ? r : q_rows - 1) * K + chunk * 8;
+    for (int l = 0; l < LOADS; ++l) {
+        const uint32_t first = (w * LOADS + l) * 16;   // of P's T rows, then Q's
+        const bool of_q = first >= T;
+        const uint32_t rows = of_q ? q_rows : p_rows, r = first % T + lane / 4;
+        offset[l] = (r < rows ? r : rows - 1) * row_bytes + exchanged(r, lane % 4) * 16;
+        to[l] = lds0 + first * kTurn * 2;
     }
-    half8 v[2][PL][H];
-    const auto fetch = [&](uint32_t k0) {
+    const auto fetch = [&](uint32_t turn) {
 #pragma unroll
-        for (int o = 0; o < 2; ++o)
-#pragma unroll
-            for (int pl = 0; pl < PL; ++pl)
-#pragma unroll
-                for (int h = 0; h < H; ++h) v[o][pl][h] = *reinterpret_cast<const half8 *>(from[o][h] + pl * (o ? plane_q : plane_p) + k0);
+        for (int l = 0; l < LOADS; ++l)
+            load_to_lds((w * LOADS + l) * 16 >= T ? base_q : base_p, offset[l], turn * (kTurn * 2), to[l] + turn % kRing * (kStage<T> * 2));
     };
-    const auto put = [&](_Float16 *to) {
-#pragma unroll
-        for (int o = 0; o < 2; ++o)
-#pragma unroll
-            for (int pl = 0; pl < PL; ++pl)
-#pragma unroll
-                for (int h = 0; h < H; ++h)
-                    *reinterpret_cast<half8 *>(to + (o * PL + pl) * T * D + staged<PAIR>(row + h * (WG / CH), chunk)) = v[o][pl][h];
+    const auto wait_for = [&](uint32_t turn) {   // after the loads of `turn` up to two more turns' were asked for
+        if (turn + 2 < turns) wait_loads<2 * LOADS>();
+        else if (turn + 1 < turns) wait_loads<LOADS>();
+        else wait_loads<0>();
     };
-    fetch(0);
-    put(lds);
-    __syncthreads();
-    int at = 0;
-    for (uint32_t k0 = 0; k0 < K; k0 += D) {
-        const bool more = k0 + D < K;
-        if (more) fetch(k0 + D);
-        const _Float16 *s = lds + at;
+    half8 a[2][FI], b[2][FJ];
+    const auto read = [&](uint32_t turn) {
+        const _Float16 *s = lds + turn % kRing * kStage<T>;
 #pragma unroll
-        for (int k = 0; k < D / 8; k += 2) {
-            half8 a[PL][FI], b[PL][FJ];
+        for (int h = 0; h < 2; ++h) {
 #pragma unroll
-            for (int pl = 0; pl < PL; ++pl) {
-#pragma unroll
-                for (int i = 0; i < FI; ++i)
-                    a[pl][i] = *reinterpret_cast<const half8 *>(s + pl * T * D + staged<PAIR>(wi + i * 32 + lane % 32, k + lane / 32));
-#pragma unroll
-                for (int j = 0; j < FJ; ++j)
-                    b[pl][j] = *reinterpret_cast<const half8 *>(s + (PL + pl) * T * D + staged<PAIR>(wj + j * 32 + lane % 32, k + lane / 32));
-            }
-            if (PAIR) {   // the small products first
-#pragma unroll
-                for (int i = 0; i < FI; ++i)
-#pragma unroll
-                    for (int j = 0; j < FJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[0][i], b[PL - 1][j], acc[i][j], 0, 0, 0);
-#pragma unroll
-                for (int i = 0; i < FI; ++i)
-#pragma unroll
-                    for (int j = 0; j < FJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[PL - 1][i], b[0][j], acc[i][j], 0, 0, 0);
-            }
+            for (int j = 0; j < FJ; ++j)
+                b[h][j] = *reinterpret_cast<const half8 *>(s + (T + wj + j * 32 + lane % 32) * kTurn + exchanged(lane % 32, h * 2 + lane / 32) * 8);
 #pragma unroll
             for (int i = 0; i < FI; ++i)
-#pragma unroll
-                for (int j = 0; j < FJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[0][i], b[0][j], acc[i][j], 0, 0, 0);
+                a[h][i] = *reinterpret_cast<const half8 *>(s + (wi + i * 32 + lane % 32) * kTurn + exchanged(lane % 32, h * 2 + lane / 32) * 8);
         }
-        at ^= kStage<T>;
-        if (more) put(lds + at);
-        __syncthreads();
+    };
+    const auto mac = [&](int ha, int hb) {
+#pragma unroll
+        for (int i = 0; i < FI; ++i)
+#pragma unroll
+            for (int j = 0; j < FJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[ha][i], b[hb][j], acc[i][j], 0, 0, 0);
+    };
+    const auto products = [&]() {
+        if (PAIR) {   // a[0], b[0] the high parts: the small products first
+            mac(0, 1);
+            mac(1, 0);
+            mac(0, 0);
+        } else {
+            mac(0, 0);
+            mac(1, 1);
+        }
+    };
+#pragma unroll
+    for (uint32_t t = 0; t < 3; ++t)
+        if (t < turns) fetch(t);
+    if (kPhases) {
+        const bool second = w >= W / 2;
+        wait_for(0);
+        meet();
+        if (second) meet();
+        for (uint32_t t = 0; t < turns; ++t) {
+            __builtin_amdgcn_sched_barrier(0);
+            read(t);
+            if (t + 3 < turns) fetch(t + 3);
+            if (second && t + 1 < turns) wait_for(t + 1);
+            meet();
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_setprio(1);
+            products();
+            __builtin_amdgcn_s_setprio(0);
+            __builtin_amdgcn_sched_barrier(0);
+            if (!second && t + 1 < turns) wait_for(t + 1);
+            meet();
+        }
+        if (!second) meet();
+    } else {
+        for (uint32_t t = 0; t < turns; ++t) {
+            wait_for(t);
+            meet();
+            read(t);
+            if (t + 3 < turns) fetch(t + 3);
+            products();
+        }
     }
+    __syncthreads();
 }
 
 // Eight results next to each other in a row of the caller's matrix.
@@ -280,12 +335,12 @@ __global__ __launch_bounds__(kThreads<T>, T == 128 ? 2 : 1) void k_ortho_product
     constexpr int PL = PAIR ? 2 : 1, WG = kThreads<T>, FI = Shape<T>::FI, FJ = Shape<T>::FJ;
     // The results go through LDS in blocks of 64 x 64: a wavefront's own, one after the other, or the workgroup's only one.
     constexpr int kTeam = T == 64 ? WG : 64, kFolds = WG / kTeam, kBlocks = T == 256 ? 2 : 1;
-    constexpr size_t kBytes = sizeof(_Float16) * 2 * kStage<T>, kFold = sizeof(float) * kFolds * 64 * kPitch;
+    constexpr size_t kBytes = sizeof(_Float16) * kRing * kStage<T>, kFold = sizeof(float) * kFolds * 64 * kPitch;
     __shared__ __attribute__((aligned(16))) unsigned char lds[kBytes > kFold ? kBytes : kFold];
     const TileDev t = OP == GRAM || OP == SQUARE ? lay.gram[blockIdx.x] : lay.product[blockIdx.x];
     const MatDev &m = lay.mats[t.mat];
     const uint32_t K = OP == GRAM ? m.Np : m.Mp, cols = OP == PRODUCT || OP == LAST ? m.Np : m.Mp;
-    const uint64_t plane_x = (uint64_t)m.Mp * m.Np, plane_a = (uint64_t)m.Mp * m.Mp;
+    const uint64_t plane_x = (uint64_t)m.Mp * m.Np;
     _Float16 *x = c.planes + m.x, *xt = c.planes + m.xt + turn * PL * plane_x, *xt_next = c.planes + m.xt + (turn ^ 1u) * PL * plane_x;
     _Float16 *a = c.planes + m.a, *b = c.planes + m.b;
     float *diag_a = c.diagonals + m.diag, *diag_b = diag_a + m.Mp;
@@ -293,8 +348,8 @@ __global__ __launch_bounds__(kThreads<T>, T == 128 ? 2 : 1) void k_ortho_product
     const _Float16 *q = OP == GRAM ? x : OP == SQUARE ? a : xt;
 
     float16v acc[FI][FJ] = {};
-    multiply<PAIR, T>(p + (uint64_t)t.i * T * K, q + (uint64_t)t.j * T * K, m.Mp - t.i * T, cols - t.j * T, OP == GRAM ? plane_x : plane_a,
-                      OP == SQUARE ? plane_a : plane_x, K, reinterpret_cast<_Float16 *>(lds), acc);
+    multiply<PAIR, T>(p + (uint64_t)t.i * T * PL * K, q + (uint64_t)t.j * T * PL * K, m.Mp - t.i * T, cols - t.j * T, K,
+                      reinterpret_cast<_Float16 *>(lds), acc);
 
     const uint32_t lane = threadIdx.x & 63u, w = threadIdx.x >> 6, tid = threadIdx.x % kTeam;
     const uint32_t wi = w / Shape<T>::WJ * FI * 32, wj = w % Shape<T>::WJ * FJ * 32;
@@ -318,13 +373,13 @@ __global__ __launch_bounds__(kThreads<T>, T == 128 ? 2 : 1) void k_ortho_product
         for (uint32_t r = there ? tid / 8 : 64u; r < 64; r += kTeam / 8) {
             const uint32_t k = tid % 8 * 8;
             float *at = fold + r * kPitch + k;
-            const uint64_t to = (uint64_t)(i0 + r) * cols + j0 + k;
+            const uint64_t to = place<PAIR>(i0 + r, j0 + k, cols);
             float v[8];
             half8 hi = {}, lo = {};
             if (OP != GRAM) {
                 const _Float16 *old = OP == SQUARE ? a : x;
                 hi = *reinterpret_cast<const half8 *>(old + to);
-                if (PAIR || OP != SQUARE) lo = *reinterpret_cast<const half8 *>(old + (OP == SQUARE ? plane_a : plane_x) + to);
+                if (PAIR || OP != SQUARE) lo = *reinterpret_cast<const half8 *>(old + to + (PAIR ? 16 : plane_x));
             }
             const float di = OP == GRAM ? 0.f : (OP == SQUARE ? diag_a : diag_b)[i0 + r] * (1.f / kScaleX);
 #pragma unroll
@@ -361,7 +416,7 @@ __global__ __launch_bounds__(kThreads<T>, T == 128 ? 2 : 1) void k_ortho_product
             }
             _Float16 *dst = OP == GRAM ? a : OP == SQUARE ? b : x;
             *reinterpret_cast<half8 *>(dst + to) = hi;
-            if (PAIR || OP == PRODUCT) *reinterpret_cast<half8 *>(dst + (OP == PRODUCT ? plane_x : plane_a) + to) = lo;
+            if (PAIR || OP == PRODUCT) *reinterpret_cast<half8 *>(dst + to + (PAIR ? 16 : plane_x)) = lo;
         }
         if (!turned) return;   // the same for the whole workgroup
         __syncthreads();
@@ -383,9 +438,9 @@ __global__ __launch_bounds__(kThreads<T>, T == 128 ? 2 : 1) void k_ortho_product
                 lo[e] = __builtin_bit_cast(_Float16, (uint16_t)(both >> 16));
             }
             _Float16 *dst = OP == GRAM ? a : OP == SQUARE ? b : xt_next;
-            const uint64_t to = (uint64_t)(j0 + r) * m.Mp + i0 + k;
+            const uint64_t to = place<PAIR>(j0 + r, i0 + k, m.Mp);
             *reinterpret_cast<half8 *>(dst + to) = hi;
-            if (PAIR) *reinterpret_cast<half8 *>(dst + (OP == PRODUCT ? plane_x : plane_a) + to) = lo;
+            if (PAIR) *reinterpret_cast<half8 *>(dst + to + 16) = lo;
         }
     };
     finish(std::integral_constant<int, 0>{});
