@@ -86,50 +86,106 @@ bool stays_bounded(uint32_t steps, const float *coef)
     return true;
 }
 
+// What a product of tiles takes, in microseconds, measured with 4096 x 4096 values at a time: a turn of a workgroup (half as deep for
+// pairs), what comes before and behind its turns, and how many workgroups the chip has room for.
+struct Rate { double turn, pair_turn, ends; uint32_t room; };
+// What the slices of a sum take to meet: each, and for every element and slice that the last one reads.
+constexpr double kMeet = 4.0, kMeetElement = 4e-5;
+Rate rate_of(uint32_t T)
+{
+    return T == 256 ? Rate{0.96, 1.29, 12.0, 256} : T == 128 ? Rate{0.51, 0.67, 8.0, 512} : Rate{0.12, 0.14, 5.0, 256};
+}
+// Slices of a sum are worth their meeting from about so many turns on, and so many at most: the last one to come reads all their sums.
+constexpr uint32_t kLeastTurns = 16, kMostSlices = 8;
+
+enum { GRAM, SQUARE, PRODUCT };
+struct Tiles {
+    uint32_t tile = 0, parts = 0;
+    std::vector<TileDev> v;
+};
+
+uint32_t turns_of(const MatDev &m, int op, uint32_t depth) { return (op == GRAM ? m.Np : m.Mp) / depth; }
+
 // Tiles of T x T of a product over all matrices, those with the longest sums first.  Workgroups go to the eight XCDs in turn, each with
 // a cache of its own, so every eighth tile is from a neighbourhood: rows of tiles, eight tiles high, are cut into eight pieces.
-std::vector<TileDev> tiles(const std::vector<MatDev> &mats, uint32_t T, bool lower)
+std::vector<TileDev> tiles_of(const std::vector<MatDev> &mats, int op, uint32_t T, uint32_t depth)
 {
     std::vector<uint32_t> order(mats.size());
     for (uint32_t k = 0; k < order.size(); ++k) order[k] = k;
-    std::stable_sort(order.begin(), order.end(), [&](uint32_t a, uint32_t b) { return mats[a].Np > mats[b].Np; });
-    std::vector<TileDev> out;
+    std::stable_sort(order.begin(), order.end(), [&](uint32_t a, uint32_t b) { return turns_of(mats[a], op, depth) > turns_of(mats[b], op, depth); });
+    std::vector<TileDev> out, own;
     for (uint32_t k : order) {
-        const uint32_t ni = (mats[k].Mp + T - 1) / T, nj = lower ? ni : (mats[k].Np + T - 1) / T;
-        std::vector<TileDev> own;
+        const uint32_t ni = (mats[k].Mp + T - 1) / T, nj = op != PRODUCT ? ni : (mats[k].Np + T - 1) / T;
+        own.clear();
         for (uint32_t i0 = 0; i0 < ni; i0 += 8)
             for (uint32_t j = 0; j < nj; ++j)
                 for (uint32_t i = i0; i < std::min(i0 + 8, ni); ++i)
-                    if (!lower || j <= i) own.push_back({k, (uint16_t)i, (uint16_t)j});
+                    if (op == PRODUCT || j <= i) own.push_back({k, (uint16_t)i, (uint16_t)j, 0, 0, 1});
         const size_t n = own.size();
-        std::vector<size_t> start(9);
-        for (size_t x = 0; x <= 8; ++x) start[x] = (n / 8) * x + std::min<size_t>(x, n % 8);
+        size_t start[9];
+        for (size_t x = 0; x <= 8; ++x) start[x] = n / 8 * x + std::min<size_t>(x, n % 8);
         for (size_t q = 0; q < n; ++q) out.push_back(own[start[q % 8] + q / 8]);
     }
     return out;
 }
 
-// Elements either way of the tiles of a product: those with which 256 workgroups at a time are done first, by the time that a workgroup
-// takes for its sums (measured: relative to 256 x 256, a CU multiplies at 0.7 of the rate with tiles of 128, at 0.35 with tiles of 64).
-uint32_t choose_tile(const std::vector<MatDev> &mats, bool lower, bool square, std::vector<TileDev> *out)
+// The tiles from number `from` on cut into slices of about `share` turns, the longest slices first.
+Tiles cut(const std::vector<MatDev> &mats, int op, uint32_t T, uint32_t depth, const std::vector<TileDev> &v, size_t from, double share)
 {
-    uint32_t best = 0;
+    Tiles out;
+    out.tile = T;
+    out.v.assign(v.begin(), v.begin() + from);
+    const auto length = [&](const TileDev &t) { return turns_of(mats[t.mat], op, depth) / t.slices; };
+    for (size_t q = from; q < v.size(); ++q) {
+        TileDev t = v[q];
+        t.slices = (uint16_t)std::max(1.0, std::min((double)kMostSlices, std::round(turns_of(mats[t.mat], op, depth) / std::max(share, (double)kLeastTurns))));
+        t.part = out.parts;
+        if (t.slices > 1) out.parts += t.slices;
+        for (t.slice = 0; t.slice < t.slices; ++t.slice) out.v.push_back(t);
+    }
+    std::stable_sort(out.v.begin() + from, out.v.end(), [&](const TileDev &a, const TileDev &b) { return length(a) > length(b); });
+    return out;
+}
+
+// How long a product takes: every workgroup goes where there is room first.
+double time_of(const std::vector<MatDev> &mats, int op, uint32_t depth, const Tiles &t)
+{
+    const Rate rate = rate_of(t.tile);
+    const double turn = (depth == 16 ? rate.pair_turn : rate.turn) * (t.tile == 128 && t.v.size() <= rate.room / 2 ? 0.6 : 1.0);
+    std::priority_queue<double, std::vector<double>, std::greater<double>> busy;
+    double last = 0.0;
+    for (const TileDev &w : t.v) {
+        double at = turns_of(mats[w.mat], op, depth) / w.slices * turn + rate.ends;
+        if (w.slices > 1) at += kMeet + w.slices * (t.tile * t.tile * kMeetElement);
+        if (busy.size() >= rate.room) { at += busy.top(); busy.pop(); }
+        busy.push(at);
+        last = std::max(last, at);
+    }
+    return last;
+}
+
+// The tiles with which a product is done first: whole, the ones behind the last full round of workgroups cut so that they fill one, or
+// all cut to the length of an even share of the turns and to parts of it.
+Tiles choose_tiles(const std::vector<MatDev> &mats, int op, bool pair)
+{
+    const uint32_t depth = pair ? 16 : 32;
+    Tiles best;
     double least = 0.0;
     for (uint32_t T : {256u, 128u, 64u}) {
-        const std::vector<TileDev> v = tiles(mats, T, lower);
-        const double rate = T == 256 ? 1.0 : T == 128 ? 0.7 : 0.35;
-        std::priority_queue<double, std::vector<double>, std::greater<double>> busy;
-        double last = 0.0;
-        for (const TileDev &t : v) {
-            const MatDev &m = mats[t.mat];
-            const double K = lower ? (double)m.Np + (square ? m.Mp : 0.0) : (double)m.Mp;
-            double at = (K + 256.0) * T * T / rate;   // the ends of a tile take about as long as 256 more products
-            if (busy.size() >= 256) { at += busy.top(); busy.pop(); }
-            busy.push(at);
-            last = std::max(last, at);
-        }
-        if (!best || last < least) { best = T; least = last; *out = v; }
-        if (v.size() > 65536) break;   // large enough to fill the chip either way
+        const std::vector<TileDev> v = tiles_of(mats, op, T, depth);
+        const size_t room = rate_of(T).room, whole = v.size() / room * room;
+        double all = 0.0, behind = 0.0;
+        for (size_t q = 0; q < v.size(); ++q) (q < whole ? all : behind) += turns_of(mats[v[q].mat], op, depth);
+        all += behind;
+        const auto consider = [&](size_t from, double share) {
+            Tiles t = cut(mats, op, T, depth, v, from, share);
+            const double time = time_of(mats, op, depth, t);
+            if (!best.tile || time < least) { least = time; best = std::move(t); }
+        };
+        consider(v.size(), 0.0);
+        if (v.size() > 16384) break;   // fills the chip either way
+        consider(whole, behind / room);
+        for (double part : {1.0, 0.7, 0.5, 0.35, 0.25}) consider(0, part * all / room);
     }
     return best;
 }
@@ -140,7 +196,7 @@ int build_plan(uint32_t count, const co3_matrix *matrices, co3_matrix_plan *p)
     const uint32_t PL = l.products == CO3_PRODUCTS_PAIR ? 2 : 1;
     std::vector<MatDev> mats(count);
     std::vector<PartDev> parts;
-    std::vector<TileDev> pack, gram, product;
+    std::vector<TileDev> pack;
     uint64_t halves = 0, diagonals = 0;
     for (uint32_t k = 0; k < count; ++k) {
         const co3_matrix &c = matrices[k];
@@ -171,34 +227,42 @@ int build_plan(uint32_t count, const co3_matrix *matrices, co3_matrix_plan *p)
         m.nparts = (uint32_t)parts.size() - m.part;
         if (parts.size() > kMaxTiles) return CO3_ERR_CAPACITY;
         for (uint32_t i = 0; i < m.Mp / kBlock; ++i)
-            for (uint32_t j = 0; j < m.Np / kBlock; ++j) pack.push_back({k, (uint16_t)i, (uint16_t)j});
+            for (uint32_t j = 0; j < m.Np / kBlock; ++j) pack.push_back({k, (uint16_t)i, (uint16_t)j, 0, 0, 1});
         if (pack.size() > kMaxTiles) return CO3_ERR_CAPACITY;
     }
-    l.gram_tile = choose_tile(mats, true, true, &gram);
-    l.product_tile = choose_tile(mats, false, false, &product);
+    const Tiles gram = choose_tiles(mats, GRAM, PL == 2), square = choose_tiles(mats, SQUARE, PL == 2), product = choose_tiles(mats, PRODUCT, PL == 2);
+    for (const Tiles *t : {&gram, &square, &product}) {
+        if (t->v.size() > kMaxTiles) return CO3_ERR_CAPACITY;
+        l.slices = std::max(l.slices, t->parts);
+        l.slice_floats = std::max(l.slice_floats, (uint64_t)t->parts * t->tile * t->tile * (t->tile == 64 ? 4 : 1));
+    }
     l.nmat = count;
     l.nparts = (uint32_t)parts.size();
-    l.npack = (uint32_t)pack.size();
-    l.ngram = (uint32_t)gram.size();
-    l.nproduct = (uint32_t)product.size();
     l.diagonals = diagonals;
-    p->workspace_bytes = up256(parts.size() * sizeof(double)) + up256(diagonals * sizeof(float)) + halves * sizeof(_Float16);
+    p->workspace_bytes = up256(parts.size() * sizeof(double)) + up256(l.slices * sizeof(uint32_t)) + up256(l.slice_floats * sizeof(float)) +
+                         up256(diagonals * sizeof(float)) + halves * sizeof(_Float16);
 
-    const size_t at_parts = up256(mats.size() * sizeof(MatDev)), at_pack = at_parts + up256(parts.size() * sizeof(PartDev));
-    const size_t at_gram = at_pack + up256(pack.size() * sizeof(TileDev)), at_product = at_gram + up256(gram.size() * sizeof(TileDev));
-    const size_t bytes = at_product + up256(product.size() * sizeof(TileDev));
-    if (hipMalloc(&p->tables, bytes) != hipSuccess) return CO3_ERR_HIP;
+    const size_t at_parts = up256(mats.size() * sizeof(MatDev));
+    const std::vector<TileDev> *all[4] = {&pack, &gram.v, &square.v, &product.v};
+    size_t at[5] = {at_parts + up256(parts.size() * sizeof(PartDev))};
+    for (int k = 0; k < 4; ++k) at[k + 1] = at[k] + up256(all[k]->size() * sizeof(TileDev));
+    if (hipMalloc(&p->tables, at[4]) != hipSuccess) return CO3_ERR_HIP;
     unsigned char *d = static_cast<unsigned char *>(p->tables);
-    const auto copy = [&](size_t at, const auto &v) {
-        return hipMemcpy(d + at, v.data(), v.size() * sizeof(v[0]), hipMemcpyHostToDevice) == hipSuccess;
+    const auto copy = [&](size_t to, const auto &v) {
+        return hipMemcpy(d + to, v.data(), v.size() * sizeof(v[0]), hipMemcpyHostToDevice) == hipSuccess;
     };
-    if (!copy(0, mats) || !copy(at_parts, parts) || !copy(at_pack, pack) || !copy(at_gram, gram) || !copy(at_product, product))
-        return CO3_ERR_HIP;
+    if (!copy(0, mats) || !copy(at_parts, parts)) return CO3_ERR_HIP;
+    for (int k = 0; k < 4; ++k)
+        if (!copy(at[k], *all[k])) return CO3_ERR_HIP;
     l.mats = reinterpret_cast<const MatDev *>(d);
     l.parts = reinterpret_cast<const PartDev *>(d + at_parts);
-    l.pack = reinterpret_cast<const TileDev *>(d + at_pack);
-    l.gram = reinterpret_cast<const TileDev *>(d + at_gram);
-    l.product = reinterpret_cast<const TileDev *>(d + at_product);
+    const auto launch = [&](int k, uint32_t tile) {
+        return LaunchDev{reinterpret_cast<const TileDev *>(d + at[k]), (uint32_t)all[k]->size(), tile};
+    };
+    l.pack = launch(0, kBlock);
+    l.gram = launch(1, gram.tile);
+    l.square = launch(2, square.tile);
+    l.product = launch(3, product.tile);
     return CO3_OK;
 }
 
@@ -216,6 +280,10 @@ int check_call(const co3_matrix_plan *plan, uint32_t steps, const float *coeffic
     c->status = status;
     c->partial = static_cast<double *>(workspace);
     unsigned char *at = static_cast<unsigned char *>(workspace) + up256(plan->lay.nparts * sizeof(double));
+    c->counters = reinterpret_cast<uint32_t *>(at);
+    at += up256(plan->lay.slices * sizeof(uint32_t));
+    c->sums = reinterpret_cast<float *>(at);
+    at += up256(plan->lay.slice_floats * sizeof(float));
     c->diagonals = reinterpret_cast<float *>(at);
     c->planes = reinterpret_cast<_Float16 *>(at + up256(plan->lay.diagonals * sizeof(float)));
     return CO3_OK;

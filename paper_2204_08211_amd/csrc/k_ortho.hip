@@ -79,12 +79,13 @@ __device__ inline void split(float v, _Float16 &hi, _Float16 &lo)
     lo = (_Float16)(v - (float)hi);
 }
 
-// Where eight values from column k (a multiple of 8) of row r of a plane of K columns begin.  Pairs have 16 high and 16 low parts in
-// turn, so that 64 bytes of a row are what a turn of the products takes of it, in either form.
+// Where eight values from column k (a multiple of 8) of row r of a plane of K columns begin.  A plane is made of blocks of 16 rows by
+// 64 bytes, a kilobyte each, which is what a wavefront asks for with one load: 32 values, or 16 high and 16 low parts.
 template <bool PAIR>
 __device__ inline uint64_t place(uint32_t r, uint32_t k, uint32_t K)
 {
-    return PAIR ? (uint64_t)r * 2 * K + k / 16 * 32 + k % 16 : (uint64_t)r * K + k;
+    constexpr uint32_t D = PAIR ? 16 : 32;
+    return ((uint64_t)(r / 16) * (K / D) + k / D) * 512 + r % 16 * 32 + k % D;
 }
 
 // What a tile of 64 x 64 floats in LDS is read and written by: 65 words a row, so that neither eight columns of eight rows nor
@@ -97,7 +98,7 @@ __global__ __launch_bounds__(256) void k_ortho_pack(OrthoLayout lay, OrthoCall c
 {
     __shared__ double lds[4];
     __shared__ float tile[kBlock * kPitch];
-    const TileDev t = lay.pack[blockIdx.x];
+    const TileDev t = lay.pack.tiles[blockIdx.x];
     const MatDev m = lay.mats[t.mat];
     double s = 0.0;
     for (uint32_t p = threadIdx.x; p < m.nparts; p += 256) s += c.partial[m.part + p];
@@ -106,6 +107,8 @@ __global__ __launch_bounds__(256) void k_ortho_pack(OrthoLayout lay, OrthoCall c
     const double f = !finite ? (double)NAN : s > 0.0 ? (double)kScaleX / (sqrt(s) + (double)c.eps) : 0.0;
     if (!finite && t.i == 0 && t.j == 0 && threadIdx.x == 0 && c.status)
         atomicAdd(reinterpret_cast<unsigned long long *>(c.status + CO3_STAT_NONFINITE), 1ull);
+
+    for (uint32_t k = blockIdx.x * 256 + threadIdx.x; k < lay.slices; k += gridDim.x * 256) c.counters[k] = 0u;
 
     const uint32_t gr = (m.tall ? t.j : t.i) * kBlock, gc = (m.tall ? t.i : t.j) * kBlock;   // in the caller's matrix
     const uint32_t lane = threadIdx.x & 63u;
@@ -150,12 +153,13 @@ __global__ __launch_bounds__(256) void k_ortho_pack(OrthoLayout lay, OrthoCall c
 
 enum { GRAM, SQUARE, PRODUCT, LAST };
 
-// The shape of a workgroup's tile: WI x WJ wavefronts of FI x FJ fragments of 32 x 32.
+// The shape of a workgroup's tile: WI x WJ wavefronts of FI x FJ fragments of 32 x 32, KW times over: each of these groups takes every
+// KW-th turn of the sum.
 template <int T> struct Shape;
-template <> struct Shape<256> { static constexpr int WI = 2, WJ = 4, FI = 4, FJ = 2; };
-template <> struct Shape<128> { static constexpr int WI = 2, WJ = 2, FI = 2, FJ = 2; };
-template <> struct Shape<64> { static constexpr int WI = 2, WJ = 2, FI = 1, FJ = 1; };
-template <int T> constexpr int kThreads = 64 * Shape<T>::WI * Shape<T>::WJ;
+template <> struct Shape<256> { static constexpr int WI = 2, WJ = 4, FI = 4, FJ = 2, KW = 1; };
+template <> struct Shape<128> { static constexpr int WI = 2, WJ = 2, FI = 2, FJ = 2, KW = 1; };
+template <> struct Shape<64> { static constexpr int WI = 2, WJ = 2, FI = 1, FJ = 1, KW = 4; };
+template <int T> constexpr int kThreads = 64 * Shape<T>::WI * Shape<T>::WJ * Shape<T>::KW;
 // A turn takes 64 bytes of every row of P and of Q: 32 values, or 16 pairs.  LDS holds four turns.
 template <bool PAIR> constexpr int kDepth = PAIR ? 16 : 32;
 constexpr int kTurn = 32, kRing = 4;                  // fp16 numbers of a row in a turn; turns in LDS
@@ -179,7 +183,8 @@ __device__ inline void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" : : "n"
 // All wavefronts of the workgroup, each with what it asked of LDS.  (__syncthreads() would wait for the loads to LDS as well.)
 __device__ inline void meet()
 {
-    asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+    asm volatile("" : : : "memory");
+    __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0)
     __builtin_amdgcn_s_barrier();
     asm volatile("" : : : "memory");
 }
@@ -194,101 +199,92 @@ __device__ inline u32x4 buffer_of(const void *p, uint32_t bytes)
     return r;
 }
 
-// acc[i][j] += sum over k of P[i][k] Q[j][k] for a wavefront's part of the tile, from rows of K values; rows past the last are
-// the last.  Three turns are on their way to LDS while one is multiplied.  With eight wavefronts, two on a SIMD, four read
-// a turn's rows from LDS while the other four multiply, and the other way round: a wait ahead of them keeps the second half a
-// phase behind.
+// acc[i][j] += sum over k of P[i][k] Q[j][k] for a wavefront's part of the tile, from rows of K values, over `all` turns from `begin`
+// on; rows past the last are others.  Where P and Q are the same rows, they are loaded once.  While a turn is multiplied, the next one's values are read from LDS and three more are on their way to it.
 template <bool PAIR, int T>
-__device__ __forceinline__ void multiply(const _Float16 *p, const _Float16 *q, uint32_t p_rows, uint32_t q_rows, uint32_t K, _Float16 *lds,
+__device__ __forceinline__ void multiply(const _Float16 *p, const _Float16 *q, uint32_t p_rows, uint32_t q_rows, uint32_t K, uint32_t begin, uint32_t all, _Float16 *lds,
                                          float16v (&acc)[Shape<T>::FI][Shape<T>::FJ])
 {
-    constexpr int FI = Shape<T>::FI, FJ = Shape<T>::FJ, W = Shape<T>::WI * Shape<T>::WJ;
+    constexpr int FI = Shape<T>::FI, FJ = Shape<T>::FJ, W = Shape<T>::WI * Shape<T>::WJ, KW = Shape<T>::KW;
     constexpr int LOADS = 2 * T / 16 / W;   // of 16 rows each, of a wavefront in a turn
-    constexpr bool kPhases = W == 8;
-    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w = wave % W, group = wave / W;
     const int wi = w / Shape<T>::WJ * FI * 32, wj = w % Shape<T>::WJ * FJ * 32;
-    const uint32_t row_bytes = K * (PAIR ? 4u : 2u), turns = K / kDepth<PAIR>;
-    const u32x4 base_p = buffer_of(p, (p_rows < T ? p_rows : T) * row_bytes), base_q = buffer_of(q, (q_rows < T ? q_rows : T) * row_bytes);
+    const uint32_t stride = K / kDepth<PAIR> * 1024;   // bytes of 16 rows, a kilobyte a turn
+    const uint32_t turns = (all - group + KW - 1) / KW, most = (all + KW - 1) / KW;   // the group's, the first group's
+    const bool same = p == q;
+    const u32x4 base_p = buffer_of(p, (p_rows < T ? p_rows : T) / 16 * stride), base_q = buffer_of(q, (q_rows < T ? q_rows : T) / 16 * stride);
+    lds += group * kRing * kStage<T>;
     const uint32_t lds0 = (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) _Float16 *)lds);
     uint32_t offset[LOADS], to[LOADS];
 #pragma unroll
     for (int l = 0; l < LOADS; ++l) {
         const uint32_t first = (w * LOADS + l) * 16;   // of P's T rows, then Q's
         const bool of_q = first >= T;
-        const uint32_t rows = of_q ? q_rows : p_rows, r = first % T + lane / 4;
-        offset[l] = (r < rows ? r : rows - 1) * row_bytes + exchanged(r, lane % 4) * 16;
+        const uint32_t rows = of_q ? q_rows : p_rows, r = first % T;   // of which there are a multiple of 64
+        offset[l] = (r < rows ? r : rows - 16) / 16 * stride + lane / 4 * 64 + exchanged(lane / 4, lane % 4) * 16;
         to[l] = lds0 + first * kTurn * 2;
     }
-    const auto fetch = [&](uint32_t turn) {
-#pragma unroll
-        for (int l = 0; l < LOADS; ++l)
-            load_to_lds((w * LOADS + l) * 16 >= T ? base_q : base_p, offset[l], turn * (kTurn * 2), to[l] + turn % kRing * (kStage<T> * 2));
+    const auto fetch = [&](uint32_t turn, int l) __attribute__((always_inline)) {
+        const bool of_q = (w * LOADS + l) * 16 >= T;   // a wavefront's loads are of P all, or of Q
+        if (of_q && same) return;
+        load_to_lds(of_q ? base_q : base_p, offset[l], (begin + turn * KW + group) * 1024, to[l] + turn % kRing * (kStage<T> * 2));
     };
     const auto wait_for = [&](uint32_t turn) {   // after the loads of `turn` up to two more turns' were asked for
         if (turn + 2 < turns) wait_loads<2 * LOADS>();
         else if (turn + 1 < turns) wait_loads<LOADS>();
         else wait_loads<0>();
     };
-    half8 a[2][FI], b[2][FJ];
-    const auto read = [&](uint32_t turn) {
-        const _Float16 *s = lds + turn % kRing * kStage<T>;
+    half8 a[2][2][FI], b[2][2][FJ];   // of this turn and of the next
+    const int q_at = (same ? 0 : T) + wj;
+    constexpr int READS = 2 * (FI + FJ), MACS = (PAIR ? 3 : 2) * FI * FJ;
+    const auto read = [&](const _Float16 *s, int n, half8 (&av)[2][FI], half8 (&bv)[2][FJ]) __attribute__((always_inline)) {
+        const int h = n / (FI + FJ), m = n % (FI + FJ);
+        if (m < FJ) bv[h][m] = *reinterpret_cast<const half8 *>(s + (q_at + m * 32 + lane % 32) * kTurn + exchanged(lane % 32, h * 2 + lane / 32) * 8);
+        else av[h][m - FJ] = *reinterpret_cast<const half8 *>(s + (wi + (m - FJ) * 32 + lane % 32) * kTurn + exchanged(lane % 32, h * 2 + lane / 32) * 8);
+    };
+    const auto mac = [&](int n, const half8 (&av)[2][FI], const half8 (&bv)[2][FJ]) __attribute__((always_inline)) {
+        const int g = n / (FI * FJ), i = n % (FI * FJ) / FJ, j = n % FJ;
+        const int ha = PAIR ? (g == 1) : g, hb = PAIR ? (g == 0) : g;   // a pair's high parts are [0]: the small products first
+        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(av[ha][i], bv[hb][j], acc[i][j], 0, 0, 0);
+    };
+    const auto step = [&](uint32_t t, const half8 (&av)[2][FI], const half8 (&bv)[2][FJ], half8 (&an)[2][FI], half8 (&bn)[2][FJ]) __attribute__((always_inline)) {
+        if (t + 1 < turns) wait_for(t + 1);
+        meet();                                   // the next turn is there, and all have read this one
+        const _Float16 *s = lds + (t + 1) % kRing * kStage<T>;   // behind the last turn: what is left in LDS, unused
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int l = 0; l < LOADS; ++l) {
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int j = 0; j < FJ; ++j)
-                b[h][j] = *reinterpret_cast<const half8 *>(s + (T + wj + j * 32 + lane % 32) * kTurn + exchanged(lane % 32, h * 2 + lane / 32) * 8);
+            for (int n = READS * l / LOADS; n < READS * (l + 1) / LOADS; ++n) read(s, n, an, bn);
 #pragma unroll
-            for (int i = 0; i < FI; ++i)
-                a[h][i] = *reinterpret_cast<const half8 *>(s + (wi + i * 32 + lane % 32) * kTurn + exchanged(lane % 32, h * 2 + lane / 32) * 8);
+            for (int n = MACS * l / LOADS; n < MACS * (l + 1) / LOADS; ++n)
+                if (KW == 1 || t < turns) mac(n, av, bv);   // one group: an even number of turns
+            if (T > 64) {
+#pragma unroll
+                for (int n = 0; n < READS / LOADS; ++n) {   // a read behind every product, while there are reads
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            if (t + 4 < turns) fetch(t + 4, l);
         }
     };
-    const auto mac = [&](int ha, int hb) {
 #pragma unroll
-        for (int i = 0; i < FI; ++i)
+    for (uint32_t t = 0; t < kRing; ++t)
 #pragma unroll
-            for (int j = 0; j < FJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[ha][i], b[hb][j], acc[i][j], 0, 0, 0);
-    };
-    const auto products = [&]() {
-        if (PAIR) {   // a[0], b[0] the high parts: the small products first
-            mac(0, 1);
-            mac(1, 0);
-            mac(0, 0);
-        } else {
-            mac(0, 0);
-            mac(1, 1);
-        }
-    };
+        for (int l = 0; l < LOADS; ++l)
+            if (t < turns) fetch(t, l);
+    if (turns > 3) wait_loads<3 * LOADS>();
+    else if (turns > 2) wait_loads<2 * LOADS>();
+    else if (turns > 1) wait_loads<LOADS>();
+    else wait_loads<0>();
+    meet();
 #pragma unroll
-    for (uint32_t t = 0; t < 3; ++t)
-        if (t < turns) fetch(t);
-    if (kPhases) {
-        const bool second = w >= W / 2;
-        wait_for(0);
-        meet();
-        if (second) meet();
-        for (uint32_t t = 0; t < turns; ++t) {
-            __builtin_amdgcn_sched_barrier(0);
-            read(t);
-            if (t + 3 < turns) fetch(t + 3);
-            if (second && t + 1 < turns) wait_for(t + 1);
-            meet();
-            __builtin_amdgcn_sched_barrier(0);
-            __builtin_amdgcn_s_setprio(1);
-            products();
-            __builtin_amdgcn_s_setprio(0);
-            __builtin_amdgcn_sched_barrier(0);
-            if (!second && t + 1 < turns) wait_for(t + 1);
-            meet();
-        }
-        if (!second) meet();
-    } else {
-        for (uint32_t t = 0; t < turns; ++t) {
-            wait_for(t);
-            meet();
-            read(t);
-            if (t + 3 < turns) fetch(t + 3);
-            products();
-        }
+    for (int n = 0; n < READS; ++n) read(lds, n, a[0], b[0]);
+    for (uint32_t t = 0; t < most; t += 2) {   // all groups' steps: they meet in every one
+        step(t, a[0], b[0], a[1], b[1]);
+        step(t + 1, a[1], b[1], a[0], b[0]);
     }
     __syncthreads();
 }
@@ -334,10 +330,11 @@ __global__ __launch_bounds__(kThreads<T>, T == 128 ? 2 : 1) void k_ortho_product
 {
     constexpr int PL = PAIR ? 2 : 1, WG = kThreads<T>, FI = Shape<T>::FI, FJ = Shape<T>::FJ;
     // The results go through LDS in blocks of 64 x 64: a wavefront's own, one after the other, or the workgroup's only one.
-    constexpr int kTeam = T == 64 ? WG : 64, kFolds = WG / kTeam, kBlocks = T == 256 ? 2 : 1;
-    constexpr size_t kBytes = sizeof(_Float16) * kRing * kStage<T>, kFold = sizeof(float) * kFolds * 64 * kPitch;
+    constexpr int KW = Shape<T>::KW, kTeam = T == 64 ? WG : 64, kFolds = T == 64 ? KW : WG / kTeam, kBlocks = T == 256 ? 2 : 1;
+    constexpr size_t kBytes = sizeof(_Float16) * kRing * kStage<T> * KW, kFold = sizeof(float) * kFolds * 64 * kPitch;
     __shared__ __attribute__((aligned(16))) unsigned char lds[kBytes > kFold ? kBytes : kFold];
-    const TileDev t = OP == GRAM || OP == SQUARE ? lay.gram[blockIdx.x] : lay.product[blockIdx.x];
+    __shared__ uint32_t arrived;
+    const TileDev t = (OP == GRAM ? lay.gram : OP == SQUARE ? lay.square : lay.product).tiles[blockIdx.x];
     const MatDev &m = lay.mats[t.mat];
     const uint32_t K = OP == GRAM ? m.Np : m.Mp, cols = OP == PRODUCT || OP == LAST ? m.Np : m.Mp;
     const uint64_t plane_x = (uint64_t)m.Mp * m.Np;
@@ -348,12 +345,52 @@ __global__ __launch_bounds__(kThreads<T>, T == 128 ? 2 : 1) void k_ortho_product
     const _Float16 *q = OP == GRAM ? x : OP == SQUARE ? a : xt;
 
     float16v acc[FI][FJ] = {};
-    multiply<PAIR, T>(p + (uint64_t)t.i * T * PL * K, q + (uint64_t)t.j * T * PL * K, m.Mp - t.i * T, cols - t.j * T, K,
+    const uint32_t turns = K / kDepth<PAIR>;   // an even number; a slice's too
+    const uint32_t begin = turns / 2 * t.slice / t.slices * 2, end = turns / 2 * (t.slice + 1) / t.slices * 2;
+    multiply<PAIR, T>(p + (uint64_t)t.i * T * PL * K, q + (uint64_t)t.j * T * PL * K, m.Mp - t.i * T, cols - t.j * T, K, begin, end - begin,
                       reinterpret_cast<_Float16 *>(lds), acc);
+    if (t.slices > 1) {
+        // The last slice to come adds all of them up, in their order.  The sums pass the caches of the XCDs by (device-scope atomics of
+        // 8 bytes; fences would write these caches back): they are where all see them once the wait is over, and counted after that.
+        constexpr uint64_t kPlace = KW * T * T / 2;
+        uint64_t *sums = reinterpret_cast<uint64_t *>(c.sums) + t.part * kPlace + threadIdx.x;
+#pragma unroll
+        for (int i = 0; i < FI; ++i)
+#pragma unroll
+            for (int j = 0; j < FJ; ++j)
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    __hip_atomic_store(&sums[t.slice * kPlace + ((i * FJ + j) * 8 + e) * WG],
+                                       (uint64_t)__float_as_uint(acc[i][j][e * 2]) | (uint64_t)__float_as_uint(acc[i][j][e * 2 + 1]) << 32,
+                                       __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        wait_loads<0>();   // and stores
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            arrived = __hip_atomic_fetch_add(&c.counters[t.part], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            if (arrived + 1 == t.slices) __hip_atomic_store(&c.counters[t.part], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        __syncthreads();
+        if (arrived + 1 != t.slices) return;
+#pragma unroll
+        for (int i = 0; i < FI; ++i)
+#pragma unroll
+            for (int j = 0; j < FJ; ++j) acc[i][j] = float16v{};
+        for (uint32_t s = 0; s < t.slices; ++s)
+#pragma unroll
+            for (int i = 0; i < FI; ++i)
+#pragma unroll
+                for (int j = 0; j < FJ; ++j)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const uint64_t v = __hip_atomic_load(&sums[s * kPlace + ((i * FJ + j) * 8 + e) * WG], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                        acc[i][j][e * 2] += __uint_as_float((uint32_t)v);
+                        acc[i][j][e * 2 + 1] += __uint_as_float((uint32_t)(v >> 32));
+                    }
+    }
 
-    const uint32_t lane = threadIdx.x & 63u, w = threadIdx.x >> 6, tid = threadIdx.x % kTeam;
+    const uint32_t lane = threadIdx.x & 63u, w = (threadIdx.x >> 6) % (WG / 64 / KW), group = threadIdx.x / (WG / KW), tid = threadIdx.x % kTeam;
     const uint32_t wi = w / Shape<T>::WJ * FI * 32, wj = w % Shape<T>::WJ * FJ * 32;
-    float *fold = reinterpret_cast<float *>(lds) + threadIdx.x / kTeam * 64 * kPitch;
+    float *fold = reinterpret_cast<float *>(lds) + threadIdx.x / kTeam * 64 * kPitch, *own = fold + group * 64 * kPitch;
     const bool turned = OP == PRODUCT || (OP == LAST && m.tall) || ((OP == GRAM || OP == SQUARE) && t.i != t.j);
     const auto finish = [&](auto which) __attribute__((always_inline)) {
         constexpr int block = decltype(which)::value, BI = FI / kBlocks;
@@ -365,7 +402,7 @@ __global__ __launch_bounds__(kThreads<T>, T == 128 ? 2 : 1) void k_ortho_product
             for (int j = 0; j < FJ; ++j)
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
-                    fold[(in_i + i * 32 + e / 4 * 8 + lane / 32 * 4 + e % 4) * kPitch + in_j + j * 32 + lane % 32] = acc[block * BI + i][j][e];
+                    own[(in_i + i * 32 + e / 4 * 8 + lane / 32 * 4 + e % 4) * kPitch + in_j + j * 32 + lane % 32] = acc[block * BI + i][j][e];
         __syncthreads();
         const uint32_t i0 = t.i * T + (T == 64 ? 0u : wi + block * 64), j0 = t.j * T + (T == 64 ? 0u : wj);
         const bool there = i0 < m.Mp && j0 < cols;   // the same for all threads of the block
@@ -374,7 +411,13 @@ __global__ __launch_bounds__(kThreads<T>, T == 128 ? 2 : 1) void k_ortho_product
             const uint32_t k = tid % 8 * 8;
             float *at = fold + r * kPitch + k;
             const uint64_t to = place<PAIR>(i0 + r, j0 + k, cols);
-            float v[8];
+            float sum[8], v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                sum[e] = at[e];
+#pragma unroll
+                for (int g = 1; g < KW; ++g) sum[e] += at[g * 64 * kPitch + e];   // the groups' sums, in their order
+            }
             half8 hi = {}, lo = {};
             if (OP != GRAM) {
                 const _Float16 *old = OP == SQUARE ? a : x;
@@ -384,14 +427,14 @@ __global__ __launch_bounds__(kThreads<T>, T == 128 ? 2 : 1) void k_ortho_product
             const float di = OP == GRAM ? 0.f : (OP == SQUARE ? diag_a : diag_b)[i0 + r] * (1.f / kScaleX);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                if (OP == GRAM) v[e] = at[e] * (1.f / kScaleX);
+                if (OP == GRAM) v[e] = sum[e] * (1.f / kScaleX);
                 if (OP == SQUARE) {
                     const bool on = i0 + r == j0 + k + e;
                     const float d = diag_a[j0 + k + e], aij = on ? d : (float)hi[e] + (float)lo[e];
-                    v[e] = f.b * aij + f.c * (at[e] * (1.f / kScaleX) + (on ? di : di + d * (1.f / kScaleX)) * aij);
+                    v[e] = f.b * aij + f.c * (sum[e] * (1.f / kScaleX) + (on ? di : di + d * (1.f / kScaleX)) * aij);
                 }
                 if (OP == PRODUCT || OP == LAST)
-                    v[e] = f.a * ((float)hi[e] + (float)lo[e]) + (di * (PAIR ? (float)hi[e] + (float)lo[e] : (float)hi[e]) + at[e] * (1.f / kScaleB));
+                    v[e] = f.a * ((float)hi[e] + (float)lo[e]) + (di * (PAIR ? (float)hi[e] + (float)lo[e] : (float)hi[e]) + sum[e] * (1.f / kScaleB));
             }
             if (OP == LAST) {
                 if (!m.tall) store_result(lay, c, m, i0 + r, j0 + k, v);
@@ -452,8 +495,8 @@ __global__ __launch_bounds__(kThreads<T>, T == 128 ? 2 : 1) void k_ortho_product
 template <int OP, bool PAIR>
 static void product(const OrthoLayout &lay, const OrthoCall &c, const Polynomial &f, uint32_t turn, hipStream_t s)
 {
-    constexpr bool lower = OP == GRAM || OP == SQUARE;
-    const uint32_t tile = lower ? lay.gram_tile : lay.product_tile, n = lower ? lay.ngram : lay.nproduct;
+    const LaunchDev &launch = OP == GRAM ? lay.gram : OP == SQUARE ? lay.square : lay.product;
+    const uint32_t tile = launch.tile, n = launch.n;
     ProfScope prof(OP == GRAM ? K_ORTHO_GRAM : OP == SQUARE ? K_ORTHO_SQUARE : K_ORTHO_PRODUCT, s);
     if (tile == 256) k_ortho_product<OP, PAIR, 256><<<dim3(n), dim3(kThreads<256>), 0, s>>>(lay, c, f, turn);
     else if (tile == 128) k_ortho_product<OP, PAIR, 128><<<dim3(n), dim3(kThreads<128>), 0, s>>>(lay, c, f, turn);
@@ -469,7 +512,7 @@ static hipError_t iterate(const OrthoLayout &lay, const OrthoCall &c, hipStream_
     }
     {
         ProfScope prof(K_ORTHO_PACK, s);
-        k_ortho_pack<T, MUON, PAIR><<<dim3(lay.npack), dim3(256), 0, s>>>(lay, c);
+        k_ortho_pack<T, MUON, PAIR><<<dim3(lay.pack.n), dim3(256), 0, s>>>(lay, c);
     }
     for (uint32_t k = 0; k < c.steps; ++k) {
         const Polynomial f = {c.coefficients[3 * k], c.coefficients[3 * k + 1], c.coefficients[3 * k + 2]};

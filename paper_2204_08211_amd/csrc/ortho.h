@@ -23,10 +23,17 @@ struct MatDev {
     uint32_t tall;              // X is the transpose
 };
 
-// One workgroup's tile of a launch over all matrices.
+// One workgroup's tile of a launch over all matrices, or a slice of its sum: the slices' sums meet in places part .. of the
+// workspace, counted at the first one's counter.
 struct TileDev {
     uint32_t mat;
     uint16_t i, j;
+    uint32_t part;
+    uint16_t slice, slices;
+};
+struct LaunchDev {
+    const TileDev *tiles;
+    uint32_t n, tile;           // tiles; elements either way of one: 64, 128 or 256
 };
 // One workgroup's part of a sum of squares: `lines` lines of `len` elements, from element `at` of the matrix on.
 struct PartDev {
@@ -39,9 +46,10 @@ constexpr uint32_t kBlock = 64;        // what X is padded to, and a tile of the
 struct OrthoLayout {
     const MatDev *mats;
     const PartDev *parts;
-    const TileDev *pack, *gram, *product;     // tiles: of X; of A and B, the lower half; of X
-    uint32_t nmat, nparts, npack, ngram, nproduct;
-    uint32_t gram_tile, product_tile;         // elements either way of a tile: 64, 128 or 256
+    LaunchDev pack, gram, square, product;    // of X; of A's lower half; of B's lower half; of X
+    uint32_t nmat, nparts;
+    uint32_t slices;                          // counters of slices, and places for their sums
+    uint64_t slice_floats;                    // fp32 elements of these
     int32_t type, products;
     uint64_t diagonals;                       // fp32 elements of all diagonals
 };
@@ -56,6 +64,8 @@ struct OrthoCall {
     const float *coefficients; // host
     uint64_t *status;
     double *partial;           // device [nparts]
+    uint32_t *counters;        // device [slices], zero between products
+    float *sums;               // device: what the slices leave for the last one of a tile
     float *diagonals;          // device
     _Float16 *planes;          // device
 };
