@@ -5,6 +5,7 @@ kernels of the library.  There is no CPU fallback: loading fails loudly when the
 not been built (python -m paper_2204_08211_amd.build).
 """
 import ctypes as C
+import functools
 import os
 
 import numpy as np
@@ -543,10 +544,17 @@ class MatrixPlan:
             pass
 
 
+@functools.lru_cache(maxsize=64)
+def _ns_triples(triples, steps):
+    c = np.asarray(triples, dtype=np.float32)
+    return np.ascontiguousarray(np.broadcast_to(c, (steps, 3)))
+
+
 def _ns_coefficients(coefficients, steps):
     """float32 [steps][3]: one triple for all steps, or one of each."""
-    c = np.asarray(coefficients, dtype=np.float32)
-    return np.ascontiguousarray(np.broadcast_to(c, (int(steps), 3)))
+    if type(coefficients) is not tuple or not all(type(x) is float for x in coefficients):
+        coefficients = tuple(map(tuple, np.broadcast_to(np.asarray(coefficients, dtype=np.float32), (int(steps), 3)).tolist()))
+    return _ns_triples(coefficients, int(steps))
 
 
 def _matrix_vector(plan, t, name):

@@ -66,19 +66,23 @@ int check_matrices(uint32_t count, const co3_matrix *m)
     return CO3_OK;
 }
 
-// The largest s p(s) = a s + b s^3 + c s^5 for s in [0, top], and the largest |b s^2 + c s^4|; the least of the former has to be
-// above -top too, since a singular value's sign is its vector's.  Both are smooth: 4096 points are near enough for limits of this use.
+// Whether p(s) = a s + b s^3 + c s^5 stays within [-2, 2] and b s^2 + c s^4 within [-7, 7] while s goes from 0 to the largest |p| of
+// the step before (1 at first).  Their extremes are at the ends and where p' = a + 3 b t + 5 c t^2 and b + 2 c t vanish, t = s^2.
 bool stays_bounded(uint32_t steps, const float *coef)
 {
     double top = 1.0;
     for (uint32_t k = 0; k < steps; ++k) {
         const double a = coef[3 * k], b = coef[3 * k + 1], c = coef[3 * k + 2];
         if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) return false;
+        double at[4] = {top * top, -b / (2 * c), 0.0, 0.0};
+        const double root = std::sqrt(9 * b * b - 20 * a * c);   // NaN, and infinities for c = 0, are no place between the ends
+        at[2] = c != 0.0 ? (-3 * b + root) / (10 * c) : -a / (3 * b);
+        at[3] = (-3 * b - root) / (10 * c);
         double most = 0.0, factor = 0.0;
-        for (int i = 0; i <= 4096; ++i) {
-            const double s = top * i / 4096.0, s2 = s * s;
-            most = std::max(most, std::fabs(s * (a + s2 * (b + s2 * c))));
-            factor = std::max(factor, std::fabs(s2 * (b + s2 * c)));
+        for (double t : at) {
+            if (!(t > 0.0 && t <= top * top)) continue;
+            most = std::max(most, std::fabs(std::sqrt(t) * (a + t * (b + t * c))));
+            factor = std::max(factor, std::fabs(t * (b + t * c)));
         }
         if (!(most <= 2.0) || !(factor <= 7.0)) return false;
         top = most;
@@ -230,6 +234,9 @@ int build_plan(uint32_t count, const co3_matrix *matrices, co3_matrix_plan *p)
             for (uint32_t j = 0; j < m.Np / kBlock; ++j) pack.push_back({k, (uint16_t)i, (uint16_t)j, 0, 0, 1});
         if (pack.size() > kMaxTiles) return CO3_ERR_CAPACITY;
     }
+    l.small = 1;
+    for (const MatDev &m : mats) l.small &= m.M <= kSmallM && m.N <= kSmallN;
+    if (l.small) halves = diagonals = 0;
     const Tiles gram = choose_tiles(mats, GRAM, PL == 2), square = choose_tiles(mats, SQUARE, PL == 2), product = choose_tiles(mats, PRODUCT, PL == 2);
     for (const Tiles *t : {&gram, &square, &product}) {
         if (t->v.size() > kMaxTiles) return CO3_ERR_CAPACITY;
@@ -275,7 +282,7 @@ int check_call(const co3_matrix_plan *plan, uint32_t steps, const float *coeffic
     if (!workspace || !aligned(workspace, 256) || !aligned(status, 8)) return CO3_ERR_ARG;
     if (workspace_bytes < plan->workspace_bytes) return CO3_ERR_CAPACITY;
     c->steps = steps;
-    c->coefficients = coefficients;
+    std::copy(coefficients, coefficients + 3 * steps, c->coefficients);
     c->eps = eps;
     c->status = status;
     c->partial = static_cast<double *>(workspace);

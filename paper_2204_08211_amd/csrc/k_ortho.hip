@@ -16,17 +16,9 @@
 #include <type_traits>
 
 #include "co3_internal.h"
-#include "ortho.h"
-#include "tensor_types.h"
+#include "ortho_device.h"
 
 namespace co3 {
-
-typedef _Float16 half8 __attribute__((ext_vector_type(8)));
-typedef float float16v __attribute__((ext_vector_type(16)));
-
-constexpr float kScaleX = 16384.f, kScaleB = 8192.f;   // 2^14, also of A; 2^13
-
-struct Polynomial { float a, b, c; };
 
 // ---- norm and layout ----------------------------------------------------------------------------------------
 
@@ -73,12 +65,6 @@ __global__ __launch_bounds__(256) void k_ortho_norm(OrthoLayout lay, OrthoCall c
     if (threadIdx.x == 0) c.partial[blockIdx.x] = s;
 }
 
-__device__ inline void split(float v, _Float16 &hi, _Float16 &lo)
-{
-    hi = (_Float16)v;
-    lo = (_Float16)(v - (float)hi);
-}
-
 // Where eight values from column k (a multiple of 8) of row r of a plane of K columns begin.  A plane is made of blocks of 16 rows by
 // 64 bytes, a kilobyte each, which is what a wavefront asks for with one load: 32 values, or 16 high and 16 low parts.
 template <bool PAIR>
@@ -103,10 +89,8 @@ __global__ __launch_bounds__(256) void k_ortho_pack(OrthoLayout lay, OrthoCall c
     double s = 0.0;
     for (uint32_t p = threadIdx.x; p < m.nparts; p += 256) s += c.partial[m.part + p];
     s = block_sum(s, lds);
-    const bool finite = s < INFINITY;   // false for NaN too
-    const double f = !finite ? (double)NAN : s > 0.0 ? (double)kScaleX / (sqrt(s) + (double)c.eps) : 0.0;
-    if (!finite && t.i == 0 && t.j == 0 && threadIdx.x == 0 && c.status)
-        atomicAdd(reinterpret_cast<unsigned long long *>(c.status + CO3_STAT_NONFINITE), 1ull);
+    const double f = scale_of(s, c.eps);
+    if (f != f && t.i == 0 && t.j == 0 && threadIdx.x == 0) count_not_finite(c);
 
     for (uint32_t k = blockIdx.x * 256 + threadIdx.x; k < lay.slices; k += gridDim.x * 256) c.counters[k] = 0u;
 
@@ -287,37 +271,6 @@ __device__ __forceinline__ void multiply(const _Float16 *p, const _Float16 *q, u
         step(t + 1, a[1], b[1], a[0], b[0]);
     }
     __syncthreads();
-}
-
-// Eight results next to each other in a row of the caller's matrix.
-__device__ inline void store_result(const OrthoLayout &lay, const OrthoCall &c, const MatDev &m, uint32_t r, uint32_t col, const float *v)
-{
-    if (r >= m.rows || col >= m.cols) return;
-    const int n = (int)(m.cols - col);
-    const uint64_t at = m.offset + (uint64_t)r * m.ld + col;
-    const float scale = m.scale / kScaleX;
-    if (!c.out) {
-        const float keep = 1.f - c.eta * c.decay, step = c.eta * scale;
-        auto w = load_pack<float, 8>(c.model + at, n);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = w[i] * keep - step * v[i];
-        store_pack<float, 8>(c.model + at, n, w);
-    } else if (lay.type == CO3_F32) {
-        Pack<float, 8>::V o;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) o[i] = v[i] * scale;
-        store_pack<float, 8>(static_cast<float *>(c.out) + at, n, o);
-    } else if (lay.type == CO3_BF16) {
-        Pack<__bf16, 8>::V o;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) o[i] = (__bf16)(v[i] * scale);
-        store_pack<__bf16, 8>(static_cast<__bf16 *>(c.out) + at, n, o);
-    } else {
-        Pack<_Float16, 8>::V o;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) o[i] = (_Float16)(v[i] * scale);
-        store_pack<_Float16, 8>(static_cast<_Float16 *>(c.out) + at, n, o);
-    }
 }
 
 // One product of every matrix.  A and B are kept without their diagonals, which are fp32: most of a matrix near the identity is
@@ -535,6 +488,7 @@ static hipError_t iterate_of(const OrthoLayout &lay, const OrthoCall &c, hipStre
 
 hipError_t launch_orthogonalize(const OrthoLayout &lay, const OrthoCall &c, hipStream_t s)
 {
+    if (lay.small) return launch_orthogonalize_small(lay, c, s);
     return lay.products == CO3_PRODUCTS_PAIR ? iterate_of<true>(lay, c, s) : iterate_of<false>(lay, c, s);
 }
 

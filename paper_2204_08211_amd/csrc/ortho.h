@@ -48,6 +48,7 @@ struct OrthoLayout {
     const PartDev *parts;
     LaunchDev pack, gram, square, product;    // of X; of A's lower half; of B's lower half; of X
     uint32_t nmat, nparts;
+    uint32_t small;                           // all matrices are: a workgroup takes one through all steps (k_ortho_small.hip)
     uint32_t slices;                          // counters of slices, and places for their sums
     uint64_t slice_floats;                    // fp32 elements of these
     int32_t type, products;
@@ -61,7 +62,7 @@ struct OrthoCall {
     float eta, beta, decay, eps;
     int32_t nesterov;
     uint32_t steps;
-    const float *coefficients; // host
+    float coefficients[3 * CO3_MAX_NS_STEPS];
     uint64_t *status;
     double *partial;           // device [nparts]
     uint32_t *counters;        // device [slices], zero between products
@@ -70,6 +71,8 @@ struct OrthoCall {
     _Float16 *planes;          // device
 };
 hipError_t launch_orthogonalize(const OrthoLayout &lay, const OrthoCall &c, hipStream_t s);
+constexpr uint32_t kSmallM = 64, kSmallN = 128;   // the largest X of launch_orthogonalize_small
+hipError_t launch_orthogonalize_small(const OrthoLayout &lay, const OrthoCall &c, hipStream_t s);
 
 }  // namespace co3
 
