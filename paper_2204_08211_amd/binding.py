@@ -214,10 +214,19 @@ def _ptr(t):
     return None if t is None else C.c_void_p(t.data_ptr())
 
 
+_torch_c = None
+
+
 def _stream(stream=None):
-    import torch
-    s = torch.cuda.current_stream() if stream is None else stream
-    return C.c_void_p(s.cuda_stream)
+    if stream is not None:
+        return C.c_void_p(stream.cuda_stream)
+    global _torch_c
+    if _torch_c is None:
+        import torch
+        torch.cuda.current_stream()   # torch's own set-up of the device
+        _torch_c = torch._C
+    # torch.cuda.current_stream() makes a Stream object of this number, which takes longer than some kernels here
+    return C.c_void_p(_torch_c._cuda_getCurrentRawStream(_torch_c._cuda_getDevice()))
 
 
 class Plan:
@@ -501,6 +510,7 @@ MAX_NORM_COLS = 32768
 MUON_COEFFICIENTS = (3.4445, -4.7750, 2.0315)
 
 
+@functools.lru_cache(maxsize=None)
 def tensor_type(dtype):
     """CO3_F32, CO3_BF16 or CO3_F16 of a torch dtype."""
     import torch
@@ -512,13 +522,14 @@ def tensor_type(dtype):
 
 class MatrixPlan:
     """co3_matrix_plan: matrices (offset, rows, cols[, ld]) of a flat vector of `dtype`, and the factor of each one's
-    orthogonalised form (scales; None: 1).  products None: PRODUCTS_PAIR for float32, PRODUCTS_HIGH for 16-bit types."""
+    orthogonalised form (scales; None: 1).  products None: PRODUCTS_HIGH for
+    bfloat16, PRODUCTS_PAIR for the other types, whose rounding is finer than that."""
 
     def __init__(self, matrices, dtype=None, scales=None, products=None):
         import torch
         dtype = torch.float32 if dtype is None else dtype
         self.dtype, self.count = dtype, len(matrices)
-        self.products = (PRODUCTS_PAIR if dtype == torch.float32 else PRODUCTS_HIGH) if products is None else int(products)
+        self.products = (PRODUCTS_HIGH if dtype == torch.bfloat16 else PRODUCTS_PAIR) if products is None else int(products)
         scales = [1.0] * self.count if scales is None else [float(x) for x in scales]
         assert len(scales) == self.count
         table = (Matrix * self.count)()
@@ -563,8 +574,10 @@ def _matrix_vector(plan, t, name):
 
 
 def _matrix_workspace(plan, workspace, device):
-    import torch
-    return torch.empty(plan.workspace_bytes, dtype=torch.uint8, device=device) if workspace is None else workspace
+    if workspace is None:
+        import torch
+        workspace = torch.empty(plan.workspace_bytes, dtype=torch.uint8, device=device)
+    return workspace
 
 
 def co3_orthogonalize(plan, g, out=None, steps=5, coefficients=MUON_COEFFICIENTS, eps=1e-7, workspace=None, status=None,
@@ -572,8 +585,8 @@ def co3_orthogonalize(plan, g, out=None, steps=5, coefficients=MUON_COEFFICIENTS
     """out = scale * Newton-Schulz iterate of every matrix of the flat vector g (out may be g; None: a new vector, with
     zeros outside the matrices).  coefficients: (a, b, c) of every step, or `steps` triples.  status (int64
     [STATUS_WORDS], or None): matrices whose norm is not finite are added to status[STAT_NONFINITE]."""
-    import torch
     if out is None:
+        import torch
         out = torch.zeros_like(g)
     _matrix_vector(plan, g, "g")
     _matrix_vector(plan, out, "out")
@@ -601,39 +614,53 @@ def co3_muon_update(plan, g, momentum, model, eta, beta=0.95, nesterov=True, wei
 
 def _norm_rows(t, name):
     """(users, rows per user, columns, elements between rows) of a [rows, cols] or [users, rows, cols] tensor."""
-    if t.dim() not in (2, 3) or (t.stride(-1) != 1 and t.shape[-1] > 1):
-        raise ValueError(f"{name}: [rows, cols] or [users, rows, cols] with contiguous rows is taken")
-    users, rows, cols = (1, *t.shape) if t.dim() == 2 else t.shape
-    stride = t.stride(-2) if rows > 1 else t.stride(0) if t.dim() == 3 and users > 1 else cols
-    if t.dim() == 3 and users > 1 and rows > 1 and t.stride(0) != rows * stride:
+    shape = t.shape
+    if len(shape) not in (2, 3):
+        raise ValueError(f"{name}: [rows, cols] or [users, rows, cols] is taken")
+    users, rows, cols = shape if len(shape) == 3 else (1, *shape)
+    if t.is_contiguous():
+        return users, rows, cols, cols
+    stride = t.stride(-2) if rows > 1 else t.stride(0) if len(shape) == 3 and users > 1 else cols
+    if t.stride(-1) != 1 and cols > 1:
+        raise ValueError(f"{name}: rows have to be contiguous")
+    if len(shape) == 3 and users > 1 and rows > 1 and t.stride(0) != rows * stride:
         raise ValueError(f"{name}: all rows have to lie the same distance apart")
     return users, rows, cols, stride
 
 
 def _norm_vector(t, n, name):
-    import torch
-    if t is not None and (t.dtype != torch.float32 or not t.is_contiguous() or t.numel() != n):
+    if t is None:
+        return None
+    if t.dtype != _float32() or t.numel() != n or not t.is_contiguous():
         raise ValueError(f"{name}: {n} contiguous float32 elements are taken")
-    return None if t is None else t.data_ptr()
+    return t.data_ptr()
 
 
-def _like_rows(t, x, name):
+@functools.lru_cache(maxsize=1)
+def _float32():
+    import torch
+    return torch.float32
+
+
+def _rows_like(t, x, name):
+    """Elements between the rows of a tensor of x's shape and type."""
     if t.shape != x.shape or t.dtype != x.dtype:
         raise ValueError(f"{name}: the shape and type of x are taken")
+    return x.shape[-1] if t.is_contiguous() else _norm_rows(t, name)[3]
 
 
 def co3_layernorm(x, weight=None, bias=None, eps=1e-5, y=None, mean=None, rstd=None, stream=None):
     """(y, mean, rstd) of x [rows, cols] or [users, rows, cols] (float32, bfloat16, float16; rows may lie apart): y of x's
     type, mean and rstd float32 without the last dimension.  weight, bias: float32 [cols] or None.  y may be x."""
-    import torch
     users, rows, cols, stride = _norm_rows(x, "x")
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if y is None else y
-    mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if mean is None else mean
-    rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if rstd is None else rstd
-    _like_rows(y, x, "y")
+    if y is None or mean is None or rstd is None:
+        import torch
+        y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if y is None else y
+        mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if mean is None else mean
+        rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if rstd is None else rstd
     a = LayernormArgs(x.data_ptr(), y.data_ptr(), _norm_vector(weight, cols, "weight"), _norm_vector(bias, cols, "bias"),
                       _norm_vector(mean, users * rows, "mean"), _norm_vector(rstd, users * rows, "rstd"), users * rows, stride,
-                      _norm_rows(y, "y")[3], cols, tensor_type(x.dtype), float(eps), 0)
+                      _rows_like(y, x, "y"), cols, tensor_type(x.dtype), float(eps), 0)
     _check("co3_layernorm", lib().co3_layernorm(C.byref(a), _stream(stream)))
     return y, mean, rstd
 
@@ -644,32 +671,36 @@ def co3_layernorm_backward_workspace_bytes(users, rows, cols):
 
 def _grad_rows(t, users, cols, name):
     """Elements between two users' gradients."""
-    import torch
-    if t.dtype != torch.float32 or t.dim() not in (1, 2) or t.shape[-1] != cols or (t.stride(-1) != 1 and cols > 1) or \
-            (t.shape[0] if t.dim() == 2 else 1) != users:
+    shape = t.shape
+    if t.dtype != _float32() or shape[-1] != cols or (shape[0] if len(shape) == 2 else 1) != users or len(shape) > 2 or \
+            (cols > 1 and t.stride(-1) != 1):
         raise ValueError(f"{name}: float32 [users, cols] with contiguous rows is taken ([cols] for one user)")
-    return t.stride(0) if t.dim() == 2 and users > 1 else cols
+    return t.stride(0) if users > 1 else cols
 
 
 def co3_layernorm_backward(dy, x, weight, mean, rstd, dx=None, dweight=None, dbias=None, accumulate=False, workspace=None,
                            stream=None):
     """dx of co3_layernorm, and where dweight / dbias are given (float32 [users, cols], rows may lie apart: a layer's part of
     the users' gradients that co3_encode reads) the weight's gradients of every user: written, or added with accumulate."""
-    import torch
     users, rows, cols, x_stride = _norm_rows(x, "x")
-    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if dx is None else dx
-    _like_rows(dy, x, "dy")
-    _like_rows(dx, x, "dx")
-    strides = [_grad_rows(t, users, cols, name) for t, name in ((dweight, "dweight"), (dbias, "dbias")) if t is not None]
-    if len(set(strides)) > 1:
-        raise ValueError("dweight and dbias: the same distance between users is taken")
-    if workspace is None and strides:
-        workspace = torch.empty(co3_layernorm_backward_workspace_bytes(users, rows, cols), dtype=torch.uint8, device=x.device)
+    stride = cols
+    if dweight is not None:
+        stride = _grad_rows(dweight, users, cols, "dweight")
+    if dbias is not None:
+        other = _grad_rows(dbias, users, cols, "dbias")
+        if dweight is not None and other != stride:
+            raise ValueError("dweight and dbias: the same distance between users is taken")
+        stride = other
+    if dx is None or workspace is None:
+        import torch
+        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if dx is None else dx
+        if workspace is None and (dweight is not None or dbias is not None):
+            workspace = torch.empty(co3_layernorm_backward_workspace_bytes(users, rows, cols), dtype=torch.uint8, device=x.device)
     a = LayernormBackwardArgs(dy.data_ptr(), x.data_ptr(), dx.data_ptr(), _norm_vector(weight, cols, "weight"),
                               _norm_vector(mean, users * rows, "mean"), _norm_vector(rstd, users * rows, "rstd"),
                               None if dweight is None else dweight.data_ptr(), None if dbias is None else dbias.data_ptr(),
-                              strides[0] if strides else 0, rows, _norm_rows(dy, "dy")[3], x_stride, _norm_rows(dx, "dx")[3], users,
-                              cols, tensor_type(x.dtype), int(bool(accumulate)), None if workspace is None else workspace.data_ptr(),
+                              stride, rows, _rows_like(dy, x, "dy"), x_stride, _rows_like(dx, x, "dx"), users, cols,
+                              tensor_type(x.dtype), 1 if accumulate else 0, None if workspace is None else workspace.data_ptr(),
                               0 if workspace is None else workspace.numel())
     _check("co3_layernorm_backward", lib().co3_layernorm_backward(C.byref(a), _stream(stream)))
     return dx

@@ -30,6 +30,32 @@ __device__ inline float row_sum(float v, float *lds)
     return v;
 }
 
+// Two sums with one meeting of the workgroup: rows take the two places in turn, so that nobody waits for the readers of the row before.
+template <int TPR>
+__device__ inline void row_sums(float &v, float &u, float (*lds)[2])
+{
+#pragma unroll
+    for (int o = (TPR < 64 ? TPR : 64) / 2; o; o >>= 1) {
+        v += __shfl_xor(v, o);
+        u += __shfl_xor(u, o);
+    }
+    if (TPR > 64) {
+        const int w = threadIdx.x >> 6;
+        if ((threadIdx.x & 63) == 0) {
+            lds[w][0] = v;
+            lds[w][1] = u;
+        }
+        __syncthreads();
+        v = lds[0][0];
+        u = lds[0][1];
+#pragma unroll
+        for (int i = 1; i < TPR / 64; ++i) {
+            v += lds[i][0];
+            u += lds[i][1];
+        }
+    }
+}
+
 template <typename T, int TPR, int CH>
 __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_layernorm(co3_layernorm_args a)
 {
@@ -85,8 +111,8 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_layernorm(co3_layerno
 }
 
 // Slices that a user's rows are cut into, one workgroup each.  A slice leaves a row of partial sums for either gradient, 16
-// bytes a column written and read again, so it has at least 32 rows of three tensors.
-constexpr uint32_t kSliceRows = 32, kSlices = 1024;
+// bytes a column written and read again, so it has at least 16 rows of three tensors.
+constexpr uint32_t kSliceRows = 16, kSlices = 1024;
 static uint32_t backward_slices(uint32_t U, uint64_t rows)
 {
     const uint64_t most = kSlices / U > 1 ? kSlices / U : 1;
@@ -98,7 +124,7 @@ template <typename T, int TPR, int CH>
 __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_layernorm_backward(co3_layernorm_backward_args a, uint32_t slices, float *partial)
 {
     constexpr int V = kVec<T>, WG = TPR > 256 ? TPR : 256, ROWS = WG / TPR;
-    __shared__ float lds[2][WG / 64];
+    __shared__ float lds[2][WG / 64][2];
     extern __shared__ float sums[];   // [2][cols], where several rows are on their way at a time
     const uint32_t u = blockIdx.y;
     const int sub = threadIdx.x / TPR, at = (int)(threadIdx.x % TPR) * V, cols = (int)a.cols;
@@ -110,18 +136,32 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_layernorm_backward(co
     for (int c = 0; c < CH; ++c)
 #pragma unroll
         for (int i = 0; i < V; ++i) dw[c][i] = db[c][i] = 0.f;
-    for (uint64_t k = r0; k < r1; k += ROWS) {   // the same number of turns for all threads
+    typename Pack<T, V>::V px[CH], pd[CH], next_x[CH], next_d[CH];
+    float mean, rstd, next_mean = 0.f, next_rstd = 0.f;
+    const auto fetch = [&](uint64_t k) {   // a row ahead of the one that is worked on
         const bool live = k + sub < r1;
         const uint64_t r = base + (live ? k + sub : k);
         const T *x = static_cast<const T *>(a.x) + r * a.x_stride, *dy = static_cast<const T *>(a.dy) + r * a.dy_stride;
-        typename Pack<T, V>::V px[CH], pd[CH];
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int j = at + c * TPR * V;
-            px[c] = load_pack<T, V>(x + j, cols - j);
-            pd[c] = load_pack<T, V>(dy + j, live ? cols - j : 0);   // a row that is not there adds nothing
+            next_x[c] = load_pack<T, V>(x + j, cols - j);
+            next_d[c] = load_pack<T, V>(dy + j, live ? cols - j : 0);   // a row that is not there adds nothing
         }
-        const float mean = a.mean[r], rstd = a.rstd[r];
+        next_mean = a.mean[r];
+        next_rstd = a.rstd[r];
+    };
+    constexpr bool kAhead = TPR <= 512;   // workgroups of 1024 threads have half the registers
+    if (kAhead && r0 < r1) fetch(r0);
+    for (uint64_t k = r0; k < r1; k += ROWS) {   // the same number of turns for all threads
+        const bool live = k + sub < r1;
+        const uint64_t r = base + (live ? k + sub : k);
+        if (!kAhead) fetch(k);
+#pragma unroll
+        for (int c = 0; c < CH; ++c) { px[c] = next_x[c]; pd[c] = next_d[c]; }
+        mean = next_mean;
+        rstd = next_rstd;
+        if (kAhead && k + ROWS < r1) fetch(k + ROWS);
         float xh[CH][V], t[CH][V], s1 = 0.f, s2 = 0.f;
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
@@ -142,8 +182,9 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_layernorm_backward(co
                 db[c][i] += d;
             }
         }
-        s1 = row_sum<TPR>(s1, lds[0]) * n;
-        s2 = row_sum<TPR>(s2, lds[1]) * n;
+        row_sums<TPR>(s1, s2, lds[(k - r0) / ROWS % 2]);
+        s1 *= n;
+        s2 *= n;
         if (!live) continue;
         T *dx = static_cast<T *>(a.dx) + r * a.dx_stride;
 #pragma unroll
@@ -191,19 +232,24 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_layernorm_backward(co
         }
 }
 
-// The slices' sums of a user, 64 columns of either gradient a workgroup.
-__global__ __launch_bounds__(256) void k_layernorm_grad(co3_layernorm_backward_args a, uint32_t slices, const float *partial)
+// The slices' sums of a user, 64 columns of either gradient a workgroup: a wavefront takes every sixteenth slice.
+__global__ __launch_bounds__(1024) void k_layernorm_grad(co3_layernorm_backward_args a, uint32_t slices, const float *partial)
 {
-    __shared__ float part[4][64];
+    __shared__ float part[16][64];
     const uint32_t u = blockIdx.y, lane = threadIdx.x & 63u, w = threadIdx.x >> 6;
     const uint64_t c = (uint64_t)blockIdx.x * 64 + lane, cols = a.cols;   // dweight's columns, then dbias's
     float s = 0.f;
-    if (c < 2 * cols)
-        for (uint32_t p = w; p < slices; p += 4) s += partial[((uint64_t)u * slices + p) * 2 * cols + c];
+    if (c < 2 * cols) {
+        const float *p = partial + (uint64_t)u * slices * 2 * cols + c;
+#pragma unroll 8
+        for (uint32_t k = w; k < slices; k += 16) s += p[k * 2 * cols];
+    }
     part[w][lane] = s;
     __syncthreads();
     if (w || c >= 2 * cols) return;
-    s = part[0][lane] + part[1][lane] + part[2][lane] + part[3][lane];
+    s = 0.f;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) s += part[k][lane];
     float *out = c < cols ? a.dweight : a.dbias;
     if (!out) return;
     out += u * a.grad_stride + (c < cols ? c : c - cols);
@@ -253,6 +299,7 @@ static void backward_of(const co3_layernorm_backward_args &a, uint32_t slices, f
     else if (packs <= 256) backward<T, 64, 4>(a, slices, partial, s);
     else if (packs <= 512) backward<T, 256, 2>(a, slices, partial, s);
     else if (packs <= 1024) backward<T, 256, 4>(a, slices, partial, s);
+    else if (packs <= 2048) backward<T, 512, 4>(a, slices, partial, s);
     else if (packs <= 4096) backward<T, 1024, 4>(a, slices, partial, s);
     else backward<T, 1024, 8>(a, slices, partial, s);
 }
@@ -286,7 +333,7 @@ hipError_t launch_layernorm_backward(const co3_layernorm_backward_args &a, hipSt
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     if (grads && slices > 1) {
         ProfScope prof(K_LAYERNORM_GRAD, s);
-        k_layernorm_grad<<<dim3((2 * a.cols + 63) / 64, a.U), dim3(256), 0, s>>>(a, slices, partial);
+        k_layernorm_grad<<<dim3((2 * a.cols + 63) / 64, a.U), dim3(1024), 0, s>>>(a, slices, partial);
     }
     return hipGetLastError();
 }
