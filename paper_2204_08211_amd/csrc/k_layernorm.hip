@@ -112,7 +112,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_layernorm(co3_layerno
 
 // Slices that a user's rows are cut into, one workgroup each.  A slice leaves a row of partial sums for either gradient, 16
 // bytes a column written and read again, so it has at least 16 rows of three tensors.
-constexpr uint32_t kSliceRows = 16, kSlices = 1024;
+constexpr uint32_t kSliceRows = 16, kSlices = 512;
 static uint32_t backward_slices(uint32_t U, uint64_t rows)
 {
     const uint64_t most = kSlices / U > 1 ? kSlices / U : 1;
@@ -136,49 +136,40 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_layernorm_backward(co
     for (int c = 0; c < CH; ++c)
 #pragma unroll
         for (int i = 0; i < V; ++i) dw[c][i] = db[c][i] = 0.f;
-    typename Pack<T, V>::V px[CH], pd[CH], next_x[CH], next_d[CH];
-    float mean, rstd, next_mean = 0.f, next_rstd = 0.f;
-    const auto fetch = [&](uint64_t k) {   // a row ahead of the one that is worked on
-        const bool live = k + sub < r1;
-        const uint64_t r = base + (live ? k + sub : k);
-        const T *x = static_cast<const T *>(a.x) + r * a.x_stride, *dy = static_cast<const T *>(a.dy) + r * a.dy_stride;
+    constexpr bool kKeep = TPR <= 512;   // workgroups of 1024 threads have half the registers: they read the weights with every row
+    typename Pack<float, V>::V w[kKeep ? CH : 1];
 #pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            const int j = at + c * TPR * V;
-            next_x[c] = load_pack<T, V>(x + j, cols - j);
-            next_d[c] = load_pack<T, V>(dy + j, live ? cols - j : 0);   // a row that is not there adds nothing
-        }
-        next_mean = a.mean[r];
-        next_rstd = a.rstd[r];
-    };
-    constexpr bool kAhead = TPR <= 512;   // workgroups of 1024 threads have half the registers
-    if (kAhead && r0 < r1) fetch(r0);
+    for (int c = 0; c < (kKeep ? CH : 1); ++c) {
+        const int j = at + c * TPR * V;
+#pragma unroll
+        for (int i = 0; i < V; ++i) w[c][i] = 1.f;
+        if (a.weight && kKeep) w[c] = load_pack<float, V>(a.weight + j, cols - j);
+    }
     for (uint64_t k = r0; k < r1; k += ROWS) {   // the same number of turns for all threads
         const bool live = k + sub < r1;
         const uint64_t r = base + (live ? k + sub : k);
-        if (!kAhead) fetch(k);
-#pragma unroll
-        for (int c = 0; c < CH; ++c) { px[c] = next_x[c]; pd[c] = next_d[c]; }
-        mean = next_mean;
-        rstd = next_rstd;
-        if (kAhead && k + ROWS < r1) fetch(k + ROWS);
-        float xh[CH][V], t[CH][V], s1 = 0.f, s2 = 0.f;
+        const T *x = static_cast<const T *>(a.x) + r * a.x_stride, *dy = static_cast<const T *>(a.dy) + r * a.dy_stride;
+        typename Pack<T, V>::V px[CH], pd[CH];
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int j = at + c * TPR * V;
-            typename Pack<float, V>::V w;
+            px[c] = load_pack<T, V>(x + j, cols - j);
+            pd[c] = load_pack<T, V>(dy + j, live ? cols - j : 0);   // a row that is not there adds nothing
+        }
+        const float mean = a.mean[r], rstd = a.rstd[r];
+        float s1 = 0.f, s2 = 0.f;
 #pragma unroll
-            for (int i = 0; i < V; ++i) w[i] = 1.f;
-            if (a.weight) w = load_pack<float, V>(a.weight + j, cols - j);
+        for (int c = 0; c < CH; ++c) {
+            const int j = at + c * TPR * V;
+            typename Pack<float, V>::V wc = w[kKeep ? c : 0];
+            if (a.weight && !kKeep) wc = load_pack<float, V>(a.weight + j, cols - j);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                const float d = (float)pd[c][i];
-                const bool in = live && j + i < cols;
-                xh[c][i] = in ? ((float)px[c][i] - mean) * rstd : 0.f;
-                t[c][i] = d * w[i];
-                s1 += t[c][i];
-                s2 += t[c][i] * xh[c][i];
-                dw[c][i] += d * xh[c][i];
+                const float d = (float)pd[c][i], t = d * wc[i];
+                const float xh = live && j + i < cols ? ((float)px[c][i] - mean) * rstd : 0.f;
+                s1 += t;
+                s2 += t * xh;
+                dw[c][i] += d * xh;
                 db[c][i] += d;
             }
         }
@@ -188,12 +179,19 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_layernorm_backward(co
         if (!live) continue;
         T *dx = static_cast<T *>(a.dx) + r * a.dx_stride;
 #pragma unroll
+        for (int c = 0; c < CH; ++c) asm volatile("" : "+v"(px[c]), "+v"(pd[c]));   // xh and t are computed once more: no registers for them
+#pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int j = at + c * TPR * V;
             if (j >= cols) break;
             typename Pack<T, V>::V p;
+            typename Pack<float, V>::V wc = w[kKeep ? c : 0];
+            if (a.weight && !kKeep) wc = load_pack<float, V>(a.weight + j, cols - j);
 #pragma unroll
-            for (int i = 0; i < V; ++i) p[i] = (T)(rstd * (t[c][i] - s1 - xh[c][i] * s2));
+            for (int i = 0; i < V; ++i) {
+                const float xh = ((float)px[c][i] - mean) * rstd;
+                p[i] = (T)(rstd * ((float)pd[c][i] * wc[i] - s1 - xh * s2));
+            }
             store_pack<T, V>(dx + j, cols - j, p);
         }
     }
