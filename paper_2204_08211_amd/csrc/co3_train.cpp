@@ -92,19 +92,18 @@ bool stays_bounded(uint32_t steps, const float *coef)
 
 // What a product of tiles takes, in microseconds, measured with 4096 x 4096 values at a time: a turn of a workgroup (half as deep for
 // pairs), what comes before and behind its turns, and how many workgroups the chip has room for.
-struct Rate { double turn, pair_turn, ends; uint32_t room; };
-// What the slices of a sum take to meet: each, and for every element and slice that the last one reads.
-constexpr double kMeet = 4.0, kMeetElement = 4e-5;
-Rate rate_of(uint32_t T)
-{
-    return T == 256 ? Rate{0.96, 1.29, 12.0, 256} : T == 128 ? Rate{0.51, 0.67, 8.0, 512} : Rate{0.12, 0.14, 5.0, 256};
-}
-// Slices of a sum are worth their meeting from about so many turns on, and so many at most: the last one to come reads all their sums.
-constexpr uint32_t kLeastTurns = 16, kMostSlices = 8;
+// What the slices of a sum take to meet, and what the last one takes for each of them, is the last two.
+struct Rate { uint32_t form, tile, groups; double turn, pair_turn, ends; uint32_t room; double meet, slice; };
+constexpr Rate kRates[] = {{256, 256, 1, 0.96, 1.29, 12.0, 256, 6.0, 4.0},
+                           {128, 128, 1, 0.51, 0.67, 8.0, 512, 5.0, 2.0},
+                           {kForm128Twice, 128, 2, 0.25, 0.35, 8.0, 256, 5.0, 2.5},
+                           {64, 64, 4, 0.12, 0.14, 4.0, 256, 3.5, 0.2}};
+constexpr uint32_t kLeastTurns = 16;   // of a slice
 
 enum { GRAM, SQUARE, PRODUCT };
 struct Tiles {
-    uint32_t tile = 0, parts = 0;
+    const Rate *rate = nullptr;
+    uint32_t parts = 0;
     std::vector<TileDev> v;
 };
 
@@ -134,10 +133,10 @@ std::vector<TileDev> tiles_of(const std::vector<MatDev> &mats, int op, uint32_t 
 }
 
 // The tiles from number `from` on cut into slices of about `share` turns, the longest slices first.
-Tiles cut(const std::vector<MatDev> &mats, int op, uint32_t T, uint32_t depth, const std::vector<TileDev> &v, size_t from, double share)
+Tiles cut(const std::vector<MatDev> &mats, int op, const Rate &rate, uint32_t depth, const std::vector<TileDev> &v, size_t from, double share)
 {
     Tiles out;
-    out.tile = T;
+    out.rate = &rate;
     out.v.assign(v.begin(), v.begin() + from);
     const auto length = [&](const TileDev &t) { return turns_of(mats[t.mat], op, depth) / t.slices; };
     for (size_t q = from; q < v.size(); ++q) {
@@ -154,13 +153,13 @@ Tiles cut(const std::vector<MatDev> &mats, int op, uint32_t T, uint32_t depth, c
 // How long a product takes: every workgroup goes where there is room first.
 double time_of(const std::vector<MatDev> &mats, int op, uint32_t depth, const Tiles &t)
 {
-    const Rate rate = rate_of(t.tile);
-    const double turn = (depth == 16 ? rate.pair_turn : rate.turn) * (t.tile == 128 && t.v.size() <= rate.room / 2 ? 0.6 : 1.0);
+    const Rate &rate = *t.rate;
+    const double turn = depth == 16 ? rate.pair_turn : rate.turn;
     std::priority_queue<double, std::vector<double>, std::greater<double>> busy;
     double last = 0.0;
     for (const TileDev &w : t.v) {
         double at = turns_of(mats[w.mat], op, depth) / w.slices * turn + rate.ends;
-        if (w.slices > 1) at += kMeet + w.slices * (t.tile * t.tile * kMeetElement);
+        if (w.slices > 1) at += rate.meet + w.slices * rate.slice;
         if (busy.size() >= rate.room) { at += busy.top(); busy.pop(); }
         busy.push(at);
         last = std::max(last, at);
@@ -169,27 +168,30 @@ double time_of(const std::vector<MatDev> &mats, int op, uint32_t depth, const Ti
 }
 
 // The tiles with which a product is done first: whole, the ones behind the last full round of workgroups cut so that they fill one, or
-// all cut to the length of an even share of the turns and to parts of it.
+// all cut to the length of an even share of the turns, to parts of it, or to the length of the shorter ones.
 Tiles choose_tiles(const std::vector<MatDev> &mats, int op, bool pair)
 {
     const uint32_t depth = pair ? 16 : 32;
     Tiles best;
     double least = 0.0;
-    for (uint32_t T : {256u, 128u, 64u}) {
-        const std::vector<TileDev> v = tiles_of(mats, op, T, depth);
-        const size_t room = rate_of(T).room, whole = v.size() / room * room;
+    for (const Rate &rate : kRates) {
+        const std::vector<TileDev> v = tiles_of(mats, op, rate.tile, depth);
+        const size_t room = rate.room, whole = v.size() / room * room;
         double all = 0.0, behind = 0.0;
         for (size_t q = 0; q < v.size(); ++q) (q < whole ? all : behind) += turns_of(mats[v[q].mat], op, depth);
         all += behind;
         const auto consider = [&](size_t from, double share) {
-            Tiles t = cut(mats, op, T, depth, v, from, share);
+            Tiles t = cut(mats, op, rate, depth, v, from, share);
             const double time = time_of(mats, op, depth, t);
-            if (!best.tile || time < least) { least = time; best = std::move(t); }
+            if (!best.rate || time < least) { least = time; best = std::move(t); }
         };
         consider(v.size(), 0.0);
         if (v.size() > 16384) break;   // fills the chip either way
         consider(whole, behind / room);
         for (double part : {1.0, 0.7, 0.5, 0.35, 0.25}) consider(0, part * all / room);
+        uint32_t before = 0;   // no slice longer than a shorter matrix's whole sum
+        for (const TileDev &t : v)
+            if (const uint32_t n = turns_of(mats[t.mat], op, depth); n != before && (before = n) != turns_of(mats[v[0].mat], op, depth)) consider(0, n);
     }
     return best;
 }
@@ -241,7 +243,7 @@ int build_plan(uint32_t count, const co3_matrix *matrices, co3_matrix_plan *p)
     for (const Tiles *t : {&gram, &square, &product}) {
         if (t->v.size() > kMaxTiles) return CO3_ERR_CAPACITY;
         l.slices = std::max(l.slices, t->parts);
-        l.slice_floats = std::max(l.slice_floats, (uint64_t)t->parts * t->tile * t->tile * (t->tile == 64 ? 4 : 1));
+        l.slice_floats = std::max(l.slice_floats, (uint64_t)t->parts * t->rate->tile * t->rate->tile * t->rate->groups);
     }
     l.nmat = count;
     l.nparts = (uint32_t)parts.size();
@@ -263,13 +265,13 @@ int build_plan(uint32_t count, const co3_matrix *matrices, co3_matrix_plan *p)
         if (!copy(at[k], *all[k])) return CO3_ERR_HIP;
     l.mats = reinterpret_cast<const MatDev *>(d);
     l.parts = reinterpret_cast<const PartDev *>(d + at_parts);
-    const auto launch = [&](int k, uint32_t tile) {
-        return LaunchDev{reinterpret_cast<const TileDev *>(d + at[k]), (uint32_t)all[k]->size(), tile};
+    const auto launch = [&](int k, uint32_t form) {
+        return LaunchDev{reinterpret_cast<const TileDev *>(d + at[k]), (uint32_t)all[k]->size(), form};
     };
-    l.pack = launch(0, kBlock);
-    l.gram = launch(1, gram.tile);
-    l.square = launch(2, square.tile);
-    l.product = launch(3, product.tile);
+    l.pack = launch(0, 0);
+    l.gram = launch(1, gram.rate->form);
+    l.square = launch(2, square.rate->form);
+    l.product = launch(3, product.rate->form);
     return CO3_OK;
 }
 

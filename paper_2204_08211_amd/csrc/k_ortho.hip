@@ -137,17 +137,18 @@ __global__ __launch_bounds__(256) void k_ortho_pack(OrthoLayout lay, OrthoCall c
 
 enum { GRAM, SQUARE, PRODUCT, LAST };
 
-// The shape of a workgroup's tile: WI x WJ wavefronts of FI x FJ fragments of 32 x 32, KW times over: each of these groups takes every
-// KW-th turn of the sum.
-template <int T> struct Shape;
-template <> struct Shape<256> { static constexpr int WI = 2, WJ = 4, FI = 4, FJ = 2, KW = 1; };
-template <> struct Shape<128> { static constexpr int WI = 2, WJ = 2, FI = 2, FJ = 2, KW = 1; };
-template <> struct Shape<64> { static constexpr int WI = 2, WJ = 2, FI = 1, FJ = 1, KW = 4; };
-template <int T> constexpr int kThreads = 64 * Shape<T>::WI * Shape<T>::WJ * Shape<T>::KW;
+// The forms of a workgroup: a tile of T x T by WI x WJ wavefronts of FI x FJ fragments of 32 x 32, KW times over: each of these groups
+// takes every KW-th turn of the sum.  One group where there are tiles for all CUs; more of them keep more loads on their way.
+template <int F> struct Form;
+template <> struct Form<256> { static constexpr int T = 256, WI = 2, WJ = 4, FI = 4, FJ = 2, KW = 1; };
+template <> struct Form<128> { static constexpr int T = 128, WI = 2, WJ = 2, FI = 2, FJ = 2, KW = 1; };
+template <> struct Form<kForm128Twice> { static constexpr int T = 128, WI = 2, WJ = 2, FI = 2, FJ = 2, KW = 2; };
+template <> struct Form<64> { static constexpr int T = 64, WI = 2, WJ = 2, FI = 1, FJ = 1, KW = 4; };
+template <int F> constexpr int kThreads = 64 * Form<F>::WI * Form<F>::WJ * Form<F>::KW;
 // A turn takes 64 bytes of every row of P and of Q: 32 values, or 16 pairs.  LDS holds four turns.
 template <bool PAIR> constexpr int kDepth = PAIR ? 16 : 32;
 constexpr int kTurn = 32, kRing = 4;                  // fp16 numbers of a row in a turn; turns in LDS
-template <int T> constexpr int kStage = 2 * T * kTurn;   // fp16 numbers of a turn
+template <int F> constexpr int kStage = 2 * Form<F>::T * kTurn;   // fp16 numbers of a turn
 
 // Where 16 bytes of a row lie in its 64 bytes in LDS: exchanged by the row's number, so that the same 16 bytes of sixteen rows, which
 // sixteen lanes read at a time, lie in different ones of the 64 banks.
@@ -185,19 +186,19 @@ __device__ inline u32x4 buffer_of(const void *p, uint32_t bytes)
 
 // acc[i][j] += sum over k of P[i][k] Q[j][k] for a wavefront's part of the tile, from rows of K values, over `all` turns from `begin`
 // on; rows past the last are others.  Where P and Q are the same rows, they are loaded once.  While a turn is multiplied, the next one's values are read from LDS and three more are on their way to it.
-template <bool PAIR, int T>
+template <bool PAIR, int F>
 __device__ __forceinline__ void multiply(const _Float16 *p, const _Float16 *q, uint32_t p_rows, uint32_t q_rows, uint32_t K, uint32_t begin, uint32_t all, _Float16 *lds,
-                                         float16v (&acc)[Shape<T>::FI][Shape<T>::FJ])
+                                         float16v (&acc)[Form<F>::FI][Form<F>::FJ])
 {
-    constexpr int FI = Shape<T>::FI, FJ = Shape<T>::FJ, W = Shape<T>::WI * Shape<T>::WJ, KW = Shape<T>::KW;
+    constexpr int T = Form<F>::T, FI = Form<F>::FI, FJ = Form<F>::FJ, W = Form<F>::WI * Form<F>::WJ, KW = Form<F>::KW;
     constexpr int LOADS = 2 * T / 16 / W;   // of 16 rows each, of a wavefront in a turn
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w = wave % W, group = wave / W;
-    const int wi = w / Shape<T>::WJ * FI * 32, wj = w % Shape<T>::WJ * FJ * 32;
+    const int wi = w / Form<F>::WJ * FI * 32, wj = w % Form<F>::WJ * FJ * 32;
     const uint32_t stride = K / kDepth<PAIR> * 1024;   // bytes of 16 rows, a kilobyte a turn
     const uint32_t turns = (all - group + KW - 1) / KW, most = (all + KW - 1) / KW;   // the group's, the first group's
     const bool same = p == q;
     const u32x4 base_p = buffer_of(p, (p_rows < T ? p_rows : T) / 16 * stride), base_q = buffer_of(q, (q_rows < T ? q_rows : T) / 16 * stride);
-    lds += group * kRing * kStage<T>;
+    lds += group * kRing * kStage<F>;
     const uint32_t lds0 = (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) _Float16 *)lds);
     uint32_t offset[LOADS], to[LOADS];
 #pragma unroll
@@ -211,7 +212,7 @@ __device__ __forceinline__ void multiply(const _Float16 *p, const _Float16 *q, u
     const auto fetch = [&](uint32_t turn, int l) __attribute__((always_inline)) {
         const bool of_q = (w * LOADS + l) * 16 >= T;   // a wavefront's loads are of P all, or of Q
         if (of_q && same) return;
-        load_to_lds(of_q ? base_q : base_p, offset[l], (begin + turn * KW + group) * 1024, to[l] + turn % kRing * (kStage<T> * 2));
+        load_to_lds(of_q ? base_q : base_p, offset[l], (begin + turn * KW + group) * 1024, to[l] + turn % kRing * (kStage<F> * 2));
     };
     const auto wait_for = [&](uint32_t turn) {   // after the loads of `turn` up to two more turns' were asked for
         if (turn + 2 < turns) wait_loads<2 * LOADS>();
@@ -234,7 +235,7 @@ __device__ __forceinline__ void multiply(const _Float16 *p, const _Float16 *q, u
     const auto step = [&](uint32_t t, const half8 (&av)[2][FI], const half8 (&bv)[2][FJ], half8 (&an)[2][FI], half8 (&bn)[2][FJ]) __attribute__((always_inline)) {
         if (t + 1 < turns) wait_for(t + 1);
         meet();                                   // the next turn is there, and all have read this one
-        const _Float16 *s = lds + (t + 1) % kRing * kStage<T>;   // behind the last turn: what is left in LDS, unused
+        const _Float16 *s = lds + (t + 1) % kRing * kStage<F>;   // behind the last turn: what is left in LDS, unused
 #pragma unroll
         for (int l = 0; l < LOADS; ++l) {
             __builtin_amdgcn_sched_barrier(0);
@@ -273,18 +274,32 @@ __device__ __forceinline__ void multiply(const _Float16 *p, const _Float16 *q, u
     __syncthreads();
 }
 
+// Whether the workgroup is the last of a sum's slices to come, after its stores.
+__device__ inline bool last_slice(uint32_t *counter, uint32_t slices, uint32_t *arrived)
+{
+    wait_loads<0>();   // and stores
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        *arrived = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (*arrived + 1 == slices) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __syncthreads();
+    return *arrived + 1 == slices;
+}
+
 // One product of every matrix.  A and B are kept without their diagonals, which are fp32: most of a matrix near the identity is
 // there, and of its rounding.  With d for A's and e for B's diagonal:
 //   B_ij = b A_ij + c ((A A)_ij + (d_i + d_j) A_ij),  e_i = b d_i + c ((A A)_ii + d_i^2),  X <- a X + e hi(X) + B hi(X)
 // (the same X in both last terms: an error of X that B as a whole would take out stays taken out).
 // `turn`: which of the two transposes this step reads.
-template <int OP, bool PAIR, int T>
-__global__ __launch_bounds__(kThreads<T>, T == 128 ? 2 : 1) void k_ortho_product(OrthoLayout lay, OrthoCall c, Polynomial f, uint32_t turn)
+template <int OP, bool PAIR, int F>
+__global__ __launch_bounds__(kThreads<F>, F == 128 ? 2 : 1) void k_ortho_product(OrthoLayout lay, OrthoCall c, Polynomial f, uint32_t turn)
 {
-    constexpr int PL = PAIR ? 2 : 1, WG = kThreads<T>, FI = Shape<T>::FI, FJ = Shape<T>::FJ;
-    // The results go through LDS in blocks of 64 x 64: a wavefront's own, one after the other, or the workgroup's only one.
-    constexpr int KW = Shape<T>::KW, kTeam = T == 64 ? WG : 64, kFolds = T == 64 ? KW : WG / kTeam, kBlocks = T == 256 ? 2 : 1;
-    constexpr size_t kBytes = sizeof(_Float16) * kRing * kStage<T> * KW, kFold = sizeof(float) * kFolds * 64 * kPitch;
+    constexpr int T = Form<F>::T, PL = PAIR ? 2 : 1, WG = kThreads<F>, FI = Form<F>::FI, FJ = Form<F>::FJ;
+    // The results go through LDS in blocks of 64 x 64, the groups' sums each: a wavefront's own block, one after the other, or the
+    // workgroup's only one.  Its team is the wavefronts that have a part in it.
+    constexpr int KW = Form<F>::KW, kTeam = T == 64 ? WG : 64 * KW, kFolds = WG / kTeam * KW, kBlocks = T == 256 ? 2 : 1;
+    constexpr size_t kBytes = sizeof(_Float16) * kRing * kStage<F> * KW, kFold = sizeof(float) * kFolds * 64 * kPitch;
     __shared__ __attribute__((aligned(16))) unsigned char lds[kBytes > kFold ? kBytes : kFold];
     __shared__ uint32_t arrived;
     const TileDev t = (OP == GRAM ? lay.gram : OP == SQUARE ? lay.square : lay.product).tiles[blockIdx.x];
@@ -297,12 +312,14 @@ __global__ __launch_bounds__(kThreads<T>, T == 128 ? 2 : 1) void k_ortho_product
     const _Float16 *p = OP == GRAM ? x : OP == SQUARE ? a : b;
     const _Float16 *q = OP == GRAM ? x : OP == SQUARE ? a : xt;
 
+    const uint32_t lane = threadIdx.x & 63u, w = (threadIdx.x >> 6) % (WG / 64 / KW), group = threadIdx.x / (WG / KW), tid = T == 64 ? threadIdx.x : group * 64 + lane;
+    const uint32_t wi = w / Form<F>::WJ * FI * 32, wj = w % Form<F>::WJ * FJ * 32;
     float16v acc[FI][FJ] = {};
     const uint32_t turns = K / kDepth<PAIR>;   // an even number; a slice's too
     const uint32_t begin = turns / 2 * t.slice / t.slices * 2, end = turns / 2 * (t.slice + 1) / t.slices * 2;
-    multiply<PAIR, T>(p + (uint64_t)t.i * T * PL * K, q + (uint64_t)t.j * T * PL * K, m.Mp - t.i * T, cols - t.j * T, K, begin, end - begin,
+    multiply<PAIR, F>(p + (uint64_t)t.i * T * PL * K, q + (uint64_t)t.j * T * PL * K, m.Mp - t.i * T, cols - t.j * T, K, begin, end - begin,
                       reinterpret_cast<_Float16 *>(lds), acc);
-    if (t.slices > 1) {
+    if (T > 64 && t.slices > 1) {
         // The last slice to come adds all of them up, in their order.  The sums pass the caches of the XCDs by (device-scope atomics of
         // 8 bytes; fences would write these caches back): they are where all see them once the wait is over, and counted after that.
         constexpr uint64_t kPlace = KW * T * T / 2;
@@ -316,14 +333,7 @@ __global__ __launch_bounds__(kThreads<T>, T == 128 ? 2 : 1) void k_ortho_product
                     __hip_atomic_store(&sums[t.slice * kPlace + ((i * FJ + j) * 8 + e) * WG],
                                        (uint64_t)__float_as_uint(acc[i][j][e * 2]) | (uint64_t)__float_as_uint(acc[i][j][e * 2 + 1]) << 32,
                                        __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        wait_loads<0>();   // and stores
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            arrived = __hip_atomic_fetch_add(&c.counters[t.part], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            if (arrived + 1 == t.slices) __hip_atomic_store(&c.counters[t.part], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        }
-        __syncthreads();
-        if (arrived + 1 != t.slices) return;
+        if (!last_slice(c.counters + t.part, t.slices, &arrived)) return;
 #pragma unroll
         for (int i = 0; i < FI; ++i)
 #pragma unroll
@@ -341,9 +351,7 @@ __global__ __launch_bounds__(kThreads<T>, T == 128 ? 2 : 1) void k_ortho_product
                     }
     }
 
-    const uint32_t lane = threadIdx.x & 63u, w = (threadIdx.x >> 6) % (WG / 64 / KW), group = threadIdx.x / (WG / KW), tid = threadIdx.x % kTeam;
-    const uint32_t wi = w / Shape<T>::WJ * FI * 32, wj = w % Shape<T>::WJ * FJ * 32;
-    float *fold = reinterpret_cast<float *>(lds) + threadIdx.x / kTeam * 64 * kPitch, *own = fold + group * 64 * kPitch;
+    float *fold = reinterpret_cast<float *>(lds) + (T == 64 ? 0 : w) * KW * 64 * kPitch, *own = fold + group * 64 * kPitch;
     const bool turned = OP == PRODUCT || (OP == LAST && m.tall) || ((OP == GRAM || OP == SQUARE) && t.i != t.j);
     const auto finish = [&](auto which) __attribute__((always_inline)) {
         constexpr int block = decltype(which)::value, BI = FI / kBlocks;
@@ -357,6 +365,40 @@ __global__ __launch_bounds__(kThreads<T>, T == 128 ? 2 : 1) void k_ortho_product
                 for (int e = 0; e < 16; ++e)
                     own[(in_i + i * 32 + e / 4 * 8 + lane / 32 * 4 + e % 4) * kPitch + in_j + j * 32 + lane % 32] = acc[block * BI + i][j][e];
         __syncthreads();
+        bool summed = false;
+        if (T == 64 && t.slices > 1) {   // the same with the groups' sums added up first: four elements a thread
+            uint64_t *sums = reinterpret_cast<uint64_t *>(c.sums) + (uint64_t)t.part * 2048 + threadIdx.x * 2;
+            float *at = fold + threadIdx.x / 16 * kPitch + threadIdx.x % 16 * 4;
+            float v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                v[e] = at[e];
+#pragma unroll
+                for (int g = 1; g < KW; ++g) v[e] += at[g * 64 * kPitch + e];
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                __hip_atomic_store(&sums[t.slice * 2048 + h], (uint64_t)__float_as_uint(v[h * 2]) | (uint64_t)__float_as_uint(v[h * 2 + 1]) << 32,
+                                   __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            if (!last_slice(c.counters + t.part, t.slices, &arrived)) return;
+            uint64_t got[kMostSlices][2];
+#pragma unroll
+            for (uint32_t s = 0; s < kMostSlices; ++s)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    if (s < t.slices) got[s][h] = __hip_atomic_load(&sums[s * 2048 + h], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = 0.f;
+#pragma unroll
+            for (uint32_t s = 0; s < kMostSlices; ++s)
+                if (s < t.slices)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] += __uint_as_float((uint32_t)(got[s][e / 2] >> e % 2 * 32));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) at[e] = v[e];
+            summed = true;
+            __syncthreads();
+        }
         const uint32_t i0 = t.i * T + (T == 64 ? 0u : wi + block * 64), j0 = t.j * T + (T == 64 ? 0u : wj);
         const bool there = i0 < m.Mp && j0 < cols;   // the same for all threads of the block
 #pragma unroll 2
@@ -369,9 +411,9 @@ __global__ __launch_bounds__(kThreads<T>, T == 128 ? 2 : 1) void k_ortho_product
             for (int e = 0; e < 8; ++e) {
                 sum[e] = at[e];
 #pragma unroll
-                for (int g = 1; g < KW; ++g) sum[e] += at[g * 64 * kPitch + e];   // the groups' sums, in their order
+                for (int g = 1; g < KW; ++g) sum[e] += summed ? 0.f : at[g * 64 * kPitch + e];   // the groups' sums, in their order
             }
-            half8 hi = {}, lo = {};
+            half8 hi = {}, lo = {};   // what the result is added to (asked for ahead of the sums it was no faster: 17.2 -> 18.6 us)
             if (OP != GRAM) {
                 const _Float16 *old = OP == SQUARE ? a : x;
                 hi = *reinterpret_cast<const half8 *>(old + to);
@@ -449,10 +491,11 @@ template <int OP, bool PAIR>
 static void product(const OrthoLayout &lay, const OrthoCall &c, const Polynomial &f, uint32_t turn, hipStream_t s)
 {
     const LaunchDev &launch = OP == GRAM ? lay.gram : OP == SQUARE ? lay.square : lay.product;
-    const uint32_t tile = launch.tile, n = launch.n;
+    const uint32_t form = launch.form, n = launch.n;
     ProfScope prof(OP == GRAM ? K_ORTHO_GRAM : OP == SQUARE ? K_ORTHO_SQUARE : K_ORTHO_PRODUCT, s);
-    if (tile == 256) k_ortho_product<OP, PAIR, 256><<<dim3(n), dim3(kThreads<256>), 0, s>>>(lay, c, f, turn);
-    else if (tile == 128) k_ortho_product<OP, PAIR, 128><<<dim3(n), dim3(kThreads<128>), 0, s>>>(lay, c, f, turn);
+    if (form == 256) k_ortho_product<OP, PAIR, 256><<<dim3(n), dim3(kThreads<256>), 0, s>>>(lay, c, f, turn);
+    else if (form == 128) k_ortho_product<OP, PAIR, 128><<<dim3(n), dim3(kThreads<128>), 0, s>>>(lay, c, f, turn);
+    else if (form == kForm128Twice) k_ortho_product<OP, PAIR, kForm128Twice><<<dim3(n), dim3(kThreads<kForm128Twice>), 0, s>>>(lay, c, f, turn);
     else k_ortho_product<OP, PAIR, 64><<<dim3(n), dim3(kThreads<64>), 0, s>>>(lay, c, f, turn);
 }
 

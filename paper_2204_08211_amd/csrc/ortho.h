@@ -23,6 +23,11 @@ struct MatDev {
     uint32_t tall;              // X is the transpose
 };
 
+constexpr uint32_t kMostSlices = 8;    // of a sum: the last one to come reads all
+
+// The forms of a workgroup of the products (k_ortho.hip), by the elements of a tile either way; this one has two groups for 128.
+constexpr int kForm128Twice = 129;
+
 // One workgroup's tile of a launch over all matrices, or a slice of its sum: the slices' sums meet in places part .. of the
 // workspace, counted at the first one's counter.
 struct TileDev {
@@ -33,7 +38,7 @@ struct TileDev {
 };
 struct LaunchDev {
     const TileDev *tiles;
-    uint32_t n, tile;           // tiles; elements either way of one: 64, 128 or 256
+    uint32_t n, form;           // tiles; what a workgroup is: 256, 128, kForm128Twice or 64
 };
 // One workgroup's part of a sum of squares: `lines` lines of `len` elements, from element `at` of the matrix on.
 struct PartDev {
