@@ -3,8 +3,7 @@
 // The same steps, scales and diagonals as in k_ortho.hip, which says what they are.  X stays in registers in fp32, as the matrix
 // instructions leave it: a wavefront has 32 x 32 of it, a lane one column and four rows at a time.  Pairs hi + lo of X, X^T, A and B
 // (or hi alone) are in LDS, whose rows are 8 numbers longer than they need: the same 16 bytes of sixteen rows lie in different banks.
-// A's and B's tiles are computed as four 32 x 32 of two halves of the sum each; since they are symmetric, a lane's four rows of a
-// column are written as four columns of a row.
+// A and B are symmetric: a lane's four rows of a column are written as four columns of a row.
 #include "co3_internal.h"
 #include "ortho_device.h"
 
@@ -19,21 +18,22 @@ constexpr int kWaves = 8, kX = kSmallN + 8, kA = kSmallM + 8, kFlat = kSmallN + 
 
 struct Planes {
     _Float16 x[2][kSmallM * kX], xt[2][kSmallN * kA], a[2][kSmallM * kA], b[2][kSmallM * kA];
-    float flat[kSmallM * kFlat];          // X row by row, on its way in and out; the second halves of sums
+    float flat[kSmallM * kFlat];          // X row by row, on its way in and out
     float diag_a[kSmallM], diag_b[kSmallM];
     double sums[kWaves];
 };
 
-// acc = P Q^T over the 16 columns from k on, `n` of them at most and while k < end, of 32 rows of each.
-template <bool PAIR, int n>
+// acc (+)= P Q^T over up to 64 columns from k on, and to `end` at most, of 32 rows of each; `small` gets the products with low parts.
+template <bool PAIR, bool FIRST>
 __device__ inline void multiply(const _Float16 *p_hi, const _Float16 *p_lo, const _Float16 *q_hi, const _Float16 *q_lo, int ld_p, int ld_q,
-                                int k, int end, float16v &acc)
+                                int k, int end, float16v &acc, float16v (&small)[2])
 {
+    constexpr int n = 4;
     const int lane = threadIdx.x & 63, at_p = lane % 32 * ld_p + lane / 32 * 8, at_q = lane % 32 * ld_q + lane / 32 * 8;
     half8 ph[n], pl[n], qh[n], ql[n];
 #pragma unroll
     for (int i = 0; i < n; ++i) {
-        const int at = k + i * 16;   // behind the end too: rows are as long
+        const int at = k + i * 16;   // behind the end too, unused: rows are as long
         ph[i] = *reinterpret_cast<const half8 *>(p_hi + at_p + at);
         qh[i] = *reinterpret_cast<const half8 *>(q_hi + at_q + at);
         if (PAIR) {
@@ -41,18 +41,19 @@ __device__ inline void multiply(const _Float16 *p_hi, const _Float16 *p_lo, cons
             ql[i] = *reinterpret_cast<const half8 *>(q_lo + at_q + at);
         }
     }
-    float16v left, right;
 #pragma unroll
     for (int i = 0; i < n; ++i) {   // sums in turn, none of which waits for itself
         if (i && k + i * 16 >= end) break;
-        if (PAIR) left = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[i], ql[i], i ? left : float16v{}, 0, 0, 0);
-        if (PAIR) right = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl[i], qh[i], i ? right : float16v{}, 0, 0, 0);
-        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[i], qh[i], i ? acc : float16v{}, 0, 0, 0);
+        const bool none = FIRST && i == 0;
+        if (PAIR) small[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[i], ql[i], none ? float16v{} : small[0], 0, 0, 0);
+        if (PAIR) small[1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl[i], qh[i], none ? float16v{} : small[1], 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[i], qh[i], none ? float16v{} : acc, 0, 0, 0);
     }
-    if (PAIR) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) acc[e] += left[e] + right[e];
-    }
+}
+template <bool PAIR>
+__device__ inline float total(const float16v &acc, const float16v (&small)[2], int e)
+{
+    return PAIR ? acc[e] + (small[0][e] + small[1][e]) : acc[e];
 }
 
 template <bool PAIR>
@@ -122,38 +123,37 @@ __global__ __launch_bounds__(64 * kWaves) void k_ortho_small(OrthoLayout lay, Or
     const double scale = scale_of(squares, c.eps) * (double)(kX7 / kScaleX);
     if (scale != scale && tid == 0) count_not_finite(c);
 
-    const uint32_t xi = w % 2 * 32, xj = w / 2 * 32;               // the wavefront's 32 x 32 of X,
-    const uint32_t ai = w % 4 / 2 * 32, aj = w % 2 * 32, half = w / 4;   // of A and B, and which half of their sums
-    const int middle = (m.N / 2 + 15) / 16 * 16 + (m.N < 2 ? 16 : 0);   // where X's columns are halved: 16 to 64
+    // The wavefront's 32 x 32 of X, and the first four's of A and B; what lies outside the matrix is neither written nor read.
+    const uint32_t xi = w % 2 * 32, xj = w / 2 * 32, ai = w % 4 / 2 * 32, aj = w % 2 * 32;
+    const bool has_x = xi < m.M && xj < m.N, has_a = w < 4 && ai < m.M && aj < m.M;
     float x[16];
 #pragma unroll
     for (int e = 0; e < 16; ++e) x[e] = (float)((double)s.flat[(xi + e / 4 * 8 + row + e % 4) * kFlat + xj + col] * scale);
 
     for (uint32_t step = 0; step < c.steps; ++step) {
         const float fa = c.coefficients[3 * step], fb = c.coefficients[3 * step + 1], fc = c.coefficients[3 * step + 2];
+        float16v acc, small[2];
+        if (has_x) {   // X and X^T; all have read the former ones
 #pragma unroll
-        for (int e = 0; e < 16; e += 4) {   // X and X^T; all have read the former ones
-            const uint32_t r = xi + e / 4 * 8 + row, n = xj + col;
-            const float v[4] = {x[e], x[e + 1], x[e + 2], x[e + 3]};
-            put4<PAIR>(&s.xt[0][n * kA + r], &s.xt[1][n * kA + r], v);
+            for (int e = 0; e < 16; e += 4) {
+                const uint32_t r = xi + e / 4 * 8 + row, n = xj + col;
+                const float v[4] = {x[e], x[e + 1], x[e + 2], x[e + 3]};
+                put4<PAIR>(&s.xt[0][n * kA + r], &s.xt[1][n * kA + r], v);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                _Float16 h, l;
-                split(v[i], h, l);
-                s.x[0][(r + i) * kX + n] = h;
-                if (PAIR) s.x[1][(r + i) * kX + n] = l;
+                for (int i = 0; i < 4; ++i) {
+                    _Float16 h, l;
+                    split(v[i], h, l);
+                    s.x[0][(r + i) * kX + n] = h;
+                    if (PAIR) s.x[1][(r + i) * kX + n] = l;
+                }
             }
         }
         __syncthreads();
         // A
-        float16v acc;
-        multiply<PAIR, 4>(s.x[0] + ai * kX, s.x[1] + ai * kX, s.x[0] + aj * kX, s.x[1] + aj * kX, kX, kX, half * middle, half ? (int)m.N : middle, acc);
-        if (half) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) s.flat[(w % 4 * 16 + e) * 64 + lane] = acc[e];
-        }
-        __syncthreads();
-        if (!half) {
+        if (has_a) {
+            const _Float16 *ph = s.x[0] + ai * kX, *pl = s.x[1] + ai * kX, *qh = s.x[0] + aj * kX, *ql = s.x[1] + aj * kX;
+            multiply<PAIR, true>(ph, pl, qh, ql, kX, kX, 0, (int)m.N, acc, small);
+            if (m.N > 64) multiply<PAIR, false>(ph, pl, qh, ql, kX, kX, 64, (int)m.N, acc, small);
             float d = 0.f;
 #pragma unroll
             for (int e = 0; e < 16; e += 4) {
@@ -161,7 +161,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_ortho_small(OrthoLayout lay, Or
                 float v[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    v[i] = acc[e + i] + s.flat[(w * 16 + e + i) * 64 + lane];
+                    v[i] = total<PAIR>(acc, small, e + i);
                     if (ai == aj) {   // the diagonal's tiles
                         d = r + i == n ? v[i] : d;
                         v[i] = r + i == n ? 0.f : v[i];
@@ -173,13 +173,8 @@ __global__ __launch_bounds__(64 * kWaves) void k_ortho_small(OrthoLayout lay, Or
         }
         __syncthreads();
         // B
-        multiply<PAIR, 2>(s.a[0] + ai * kA, s.a[1] + ai * kA, s.a[0] + aj * kA, s.a[1] + aj * kA, kA, kA, half * 32, (int)m.M, acc);
-        if (half) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) s.flat[(w % 4 * 16 + e) * 64 + lane] = acc[e];
-        }
-        __syncthreads();
-        if (!half) {
+        if (has_a) {
+            multiply<PAIR, true>(s.a[0] + ai * kA, s.a[1] + ai * kA, s.a[0] + aj * kA, s.a[1] + aj * kA, kA, kA, 0, (int)m.M, acc, small);
             const float dn = s.diag_a[aj + col], base = fmaf(dn, fc * kInvA * 0.5f, fb * 0.5f), cc = fc * kInvA * 0.5f;
             float d_b = 0.f;
 #pragma unroll
@@ -196,7 +191,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_ortho_small(OrthoLayout lay, Or
                         a = r + i == n ? dn : a;
                         t = r + i == n ? base : t;
                     }
-                    v[i] = fmaf(t, a, cc * (acc[e + i] + s.flat[(w * 16 + e + i) * 64 + lane]));
+                    v[i] = fmaf(t, a, cc * total<PAIR>(acc, small, e + i));
                     if (ai == aj) {
                         d_b = r + i == n ? v[i] : d_b;
                         v[i] = r + i == n ? 0.f : v[i];
@@ -208,13 +203,14 @@ __global__ __launch_bounds__(64 * kWaves) void k_ortho_small(OrthoLayout lay, Or
         }
         __syncthreads();
         // X
-        acc = float16v{};
-        multiply<PAIR, 4>(s.b[0] + xi * kA, s.b[1] + xi * kA, s.xt[0] + xj * kA, s.xt[1] + xj * kA, kA, kA, 0, (int)m.M, acc);
+        if (has_x) {
+            multiply<PAIR, true>(s.b[0] + xi * kA, s.b[1] + xi * kA, s.xt[0] + xj * kA, s.xt[1] + xj * kA, kA, kA, 0, (int)m.M, acc, small);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const float d = s.diag_b[xi + e / 4 * 8 + row + e % 4];
-            const float kept = PAIR ? x[e] * fmaf(d, kInvB, fa) : fmaf(x[e], fa, (float)(_Float16)x[e] * (d * kInvB));
-            x[e] = fmaf(acc[e], kInvB, kept);
+            for (int e = 0; e < 16; ++e) {
+                const float d = s.diag_b[xi + e / 4 * 8 + row + e % 4];
+                const float kept = PAIR ? x[e] * fmaf(d, kInvB, fa) : fmaf(x[e], fa, (float)(_Float16)x[e] * (d * kInvB));
+                x[e] = fmaf(total<PAIR>(acc, small, e), kInvB, kept);
+            }
         }
         __syncthreads();
     }
