@@ -216,8 +216,7 @@ int build_plan(uint32_t count, const co3_matrix *matrices, co3_matrix_plan *p)
         m.Np = up(m.N, kBlock);
         m.diag = diagonals; diagonals += 2 * m.Mp;
         const uint64_t plane_x = (uint64_t)m.Mp * m.Np, plane_a = (uint64_t)m.Mp * m.Mp;
-        m.x = halves; halves += 2 * plane_x;
-        m.xt = halves; halves += 2 * PL * plane_x;
+        m.x = halves; halves += 4 * plane_x;
         m.a = halves; halves += PL * plane_a;
         m.b = halves; halves += PL * plane_a;
         p->elements = std::max(p->elements, end_of(c));

@@ -3,8 +3,8 @@
 //   X_0 = G / (|G|_F + eps);   A = X X^T,  B = b A + c A A,  X <- a X + B X
 //
 // A launch does one product for all matrices, a workgroup one tile: tables made with the plan say which.  A and A A are
-// symmetric: only tiles on and below the diagonal are computed, the others are written from them.  All three products
-// take their operands as rows that are contiguous along the sum (X X^T, A A^T, B (X^T)^T), so X is kept with its transpose.
+// symmetric: only tiles on and below the diagonal are computed, the others are written from them.  Their operands' rows run along
+// the sum; in B X those of X run across it, and are transposed as they are read from LDS.
 //
 // Numbers.  The matrix instructions take fp16 and add in fp32.  X, A and B are held times 2^14, 2^14 and 2^13: X's singular
 // values stay below 2 and B's below 7, so nothing overflows, and at 2^14 what matters is far from the smallest fp16 number
@@ -78,7 +78,7 @@ __device__ inline uint64_t place(uint32_t r, uint32_t k, uint32_t K)
 // eight rows of eight columns meet in a bank.
 constexpr int kPitch = 65;
 
-// X_0 and its transpose, with the padding.
+// X_0, with the padding.
 template <typename T, bool MUON, bool PAIR>
 __global__ __launch_bounds__(256) void k_ortho_pack(OrthoLayout lay, OrthoCall c)
 {
@@ -107,29 +107,21 @@ __global__ __launch_bounds__(256) void k_ortho_pack(OrthoLayout lay, OrthoCall c
         tile[r * kPitch + lane] = v;
     }
     __syncthreads();
-    const uint64_t plane = (uint64_t)m.Mp * m.Np;
-    _Float16 *x = c.planes + m.x, *xt = c.planes + m.xt;
+    _Float16 *x = c.planes + m.x;
 #pragma unroll
-    for (uint32_t pass = 0; pass < 4; ++pass) {
-        const bool across = pass & 1u;                                  // the tile's columns
-        const uint32_t r = (pass >> 1) * 32 + threadIdx.x / 8, k = threadIdx.x % 8 * 8;
+    for (uint32_t pass = 0; pass < 2; ++pass) {   // X's rows: the tile's, or its columns
+        const uint32_t r = pass * 32 + threadIdx.x / 8, k = threadIdx.x % 8 * 8;
         half8 hi, lo;
 #pragma unroll
         for (uint32_t i = 0; i < 8; ++i) {
             _Float16 h, l;
-            split(tile[across ? (k + i) * kPitch + r : r * kPitch + k + i], h, l);
+            split(tile[m.tall ? (k + i) * kPitch + r : r * kPitch + k + i], h, l);
             hi[i] = h;
             lo[i] = l;
         }
-        if (across == (m.tall != 0)) {
-            _Float16 *to = x + place<PAIR>(t.i * kBlock + r, t.j * kBlock + k, m.Np);
-            *reinterpret_cast<half8 *>(to) = hi;
-            *reinterpret_cast<half8 *>(to + (PAIR ? 16 : plane)) = lo;
-        } else {
-            _Float16 *to = xt + place<PAIR>(t.j * kBlock + r, t.i * kBlock + k, m.Mp);
-            *reinterpret_cast<half8 *>(to) = hi;
-            if (PAIR) *reinterpret_cast<half8 *>(to + 16) = lo;
-        }
+        _Float16 *to = x + place<PAIR>(t.i * kBlock + r, t.j * kBlock + k, m.Np);
+        *reinterpret_cast<half8 *>(to) = hi;
+        *reinterpret_cast<half8 *>(to + (PAIR ? 16 : (uint64_t)m.Mp * m.Np)) = lo;
     }
 }
 
@@ -165,6 +157,21 @@ __device__ inline void load_to_lds(u32x4 base, uint32_t offset, uint32_t k, uint
 template <int left>
 __device__ inline void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" : : "n"(left) : "memory"); }
 
+// 32 columns from `col` on by 16 rows of a turn's blocks in LDS, as an operand whose rows the columns are: a lane gets eight rows of a
+// column.  Sixteen lanes read four rows of sixteen columns, four next to each other each, and are given four rows of one column.
+template <bool PAIR>
+__device__ inline half8 read_down(const _Float16 *blocks, int across, int h, int col)
+{
+    typedef short short4v __attribute__((ext_vector_type(4)));
+    typedef short short8v __attribute__((ext_vector_type(8)));
+    const int lane = threadIdx.x & 63, side = lane / 16 % 2, row = lane / 32 * 8 + lane % 16 / 4, four = lane % 4 * 4;
+    const _Float16 *at = PAIR ? blocks + (col / 16 + side) * 512 + row * 32 + h * 16 + four
+                              : blocks + (h * across + col / 32) * 512 + row * 32 + side * 16 + four;
+    typedef __attribute__((address_space(3))) short4v *lds4;
+    const short4v low = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)at), high = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(at + 4 * 32));
+    return __builtin_bit_cast(half8, (short8v)__builtin_shufflevector(low, high, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
 // All wavefronts of the workgroup, each with what it asked of LDS.  (__syncthreads() would wait for the loads to LDS as well.)
 __device__ inline void meet()
 {
@@ -185,9 +192,11 @@ __device__ inline u32x4 buffer_of(const void *p, uint32_t bytes)
 }
 
 // acc[i][j] += sum over k of P[i][k] Q[j][k] for a wavefront's part of the tile, from rows of K values, over `all` turns from `begin`
-// on; rows past the last are others.  Where P and Q are the same rows, they are loaded once.  While a turn is multiplied, the next one's values are read from LDS and three more are on their way to it.
-template <bool PAIR, int F>
-__device__ __forceinline__ void multiply(const _Float16 *p, const _Float16 *q, uint32_t p_rows, uint32_t q_rows, uint32_t K, uint32_t begin, uint32_t all, _Float16 *lds,
+// on; rows past the last are others.  Where P and Q are the same rows, they are loaded once.  DOWN: Q is given by columns, as a plane of
+// K rows of `across` columns, of which the tile's are those from q_rows on.
+// While a turn is multiplied, the next one's values are read from LDS and three more are on their way to it.
+template <bool PAIR, bool DOWN, int F>
+__device__ __forceinline__ void multiply(const _Float16 *p, const _Float16 *q, uint32_t p_rows, uint32_t q_rows, uint32_t across, uint32_t K, uint32_t begin, uint32_t all, _Float16 *lds,
                                          float16v (&acc)[Form<F>::FI][Form<F>::FJ])
 {
     constexpr int T = Form<F>::T, FI = Form<F>::FI, FJ = Form<F>::FJ, W = Form<F>::WI * Form<F>::WJ, KW = Form<F>::KW;
@@ -197,7 +206,9 @@ __device__ __forceinline__ void multiply(const _Float16 *p, const _Float16 *q, u
     const uint32_t stride = K / kDepth<PAIR> * 1024;   // bytes of 16 rows, a kilobyte a turn
     const uint32_t turns = (all - group + KW - 1) / KW, most = (all + KW - 1) / KW;   // the group's, the first group's
     const bool same = p == q;
-    const u32x4 base_p = buffer_of(p, (p_rows < T ? p_rows : T) / 16 * stride), base_q = buffer_of(q, (q_rows < T ? q_rows : T) / 16 * stride);
+    constexpr uint32_t D = kDepth<PAIR>, DEEP = D / 16;      // 16 rows are a block's: of the DEEP ones of a turn, `wide` bytes each
+    const uint32_t wide = DOWN ? across / D * 1024 : 0;
+    const u32x4 base_p = buffer_of(p, (p_rows < T ? p_rows : T) / 16 * stride), base_q = buffer_of(q, DOWN ? 0 : (q_rows < T ? q_rows : T) / 16 * stride);
     lds += group * kRing * kStage<F>;
     const uint32_t lds0 = (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) _Float16 *)lds);
     uint32_t offset[LOADS], to[LOADS];
@@ -207,12 +218,18 @@ __device__ __forceinline__ void multiply(const _Float16 *p, const _Float16 *q, u
         const bool of_q = first >= T;
         const uint32_t rows = of_q ? q_rows : p_rows, r = first % T;   // of which there are a multiple of 64
         offset[l] = (r < rows ? r : rows - 16) / 16 * stride + lane / 4 * 64 + exchanged(lane / 4, lane % 4) * 16;
+        if (DOWN && of_q) {   // block r / 16 of the turn's DEEP by T / D, as it is
+            const uint32_t at = q_rows / D + r / 16 % (T / D);
+            offset[l] = r / 16 / (T / D) * wide + (at < across / D ? at : across / D - 1) * 1024 + lane * 16;
+        }
         to[l] = lds0 + first * kTurn * 2;
     }
     const auto fetch = [&](uint32_t turn, int l) __attribute__((always_inline)) {
         const bool of_q = (w * LOADS + l) * 16 >= T;   // a wavefront's loads are of P all, or of Q
         if (of_q && same) return;
-        load_to_lds(of_q ? base_q : base_p, offset[l], (begin + turn * KW + group) * 1024, to[l] + turn % kRing * (kStage<F> * 2));
+        const uint32_t n = begin + turn * KW + group;
+        if (DOWN && of_q) load_to_lds(buffer_of(q + (uint64_t)n * DEEP * (wide / 2), DEEP * wide), offset[l], 0, to[l] + turn % kRing * (kStage<F> * 2));
+        else load_to_lds(of_q ? base_q : base_p, offset[l], n * 1024, to[l] + turn % kRing * (kStage<F> * 2));
     };
     const auto wait_for = [&](uint32_t turn) {   // after the loads of `turn` up to two more turns' were asked for
         if (turn + 2 < turns) wait_loads<2 * LOADS>();
@@ -224,7 +241,8 @@ __device__ __forceinline__ void multiply(const _Float16 *p, const _Float16 *q, u
     constexpr int READS = 2 * (FI + FJ), MACS = (PAIR ? 3 : 2) * FI * FJ;
     const auto read = [&](const _Float16 *s, int n, half8 (&av)[2][FI], half8 (&bv)[2][FJ]) __attribute__((always_inline)) {
         const int h = n / (FI + FJ), m = n % (FI + FJ);
-        if (m < FJ) bv[h][m] = *reinterpret_cast<const half8 *>(s + (q_at + m * 32 + lane % 32) * kTurn + exchanged(lane % 32, h * 2 + lane / 32) * 8);
+        if (DOWN && m < FJ) bv[h][m] = read_down<PAIR>(s + T * kTurn, T / 32, h, wj + m * 32);
+        else if (m < FJ) bv[h][m] = *reinterpret_cast<const half8 *>(s + (q_at + m * 32 + lane % 32) * kTurn + exchanged(lane % 32, h * 2 + lane / 32) * 8);
         else av[h][m - FJ] = *reinterpret_cast<const half8 *>(s + (wi + (m - FJ) * 32 + lane % 32) * kTurn + exchanged(lane % 32, h * 2 + lane / 32) * 8);
     };
     const auto mac = [&](int n, const half8 (&av)[2][FI], const half8 (&bv)[2][FJ]) __attribute__((always_inline)) {
@@ -246,7 +264,7 @@ __device__ __forceinline__ void multiply(const _Float16 *p, const _Float16 *q, u
                 if (KW == 1 || t < turns) mac(n, av, bv);   // one group: an even number of turns
             if (T > 64) {
 #pragma unroll
-                for (int n = 0; n < READS / LOADS; ++n) {   // a read behind every product, while there are reads
+                for (int n = 0; n < (READS + (DOWN ? 2 * FJ : 0)) / LOADS; ++n) {   // a read behind every product, while there are reads
                     __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
                     __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
                 }
@@ -291,7 +309,7 @@ __device__ inline bool last_slice(uint32_t *counter, uint32_t slices, uint32_t *
 // there, and of its rounding.  With d for A's and e for B's diagonal:
 //   B_ij = b A_ij + c ((A A)_ij + (d_i + d_j) A_ij),  e_i = b d_i + c ((A A)_ii + d_i^2),  X <- a X + e hi(X) + B hi(X)
 // (the same X in both last terms: an error of X that B as a whole would take out stays taken out).
-// `turn`: which of the two transposes this step reads.
+// `turn`: which of the two X this step reads; it writes the other.
 template <int OP, bool PAIR, int F>
 __global__ __launch_bounds__(kThreads<F>, F == 128 ? 2 : 1) void k_ortho_product(OrthoLayout lay, OrthoCall c, Polynomial f, uint32_t turn)
 {
@@ -306,19 +324,20 @@ __global__ __launch_bounds__(kThreads<F>, F == 128 ? 2 : 1) void k_ortho_product
     const MatDev &m = lay.mats[t.mat];
     const uint32_t K = OP == GRAM ? m.Np : m.Mp, cols = OP == PRODUCT || OP == LAST ? m.Np : m.Mp;
     const uint64_t plane_x = (uint64_t)m.Mp * m.Np;
-    _Float16 *x = c.planes + m.x, *xt = c.planes + m.xt + turn * PL * plane_x, *xt_next = c.planes + m.xt + (turn ^ 1u) * PL * plane_x;
+    _Float16 *x = c.planes + m.x + turn * 2 * plane_x, *x_next = c.planes + m.x + (turn ^ 1u) * 2 * plane_x;
     _Float16 *a = c.planes + m.a, *b = c.planes + m.b;
     float *diag_a = c.diagonals + m.diag, *diag_b = diag_a + m.Mp;
     const _Float16 *p = OP == GRAM ? x : OP == SQUARE ? a : b;
-    const _Float16 *q = OP == GRAM ? x : OP == SQUARE ? a : xt;
+    const _Float16 *q = OP == GRAM ? x : OP == SQUARE ? a : x;
 
     const uint32_t lane = threadIdx.x & 63u, w = (threadIdx.x >> 6) % (WG / 64 / KW), group = threadIdx.x / (WG / KW), tid = T == 64 ? threadIdx.x : group * 64 + lane;
     const uint32_t wi = w / Form<F>::WJ * FI * 32, wj = w % Form<F>::WJ * FJ * 32;
     float16v acc[FI][FJ] = {};
     const uint32_t turns = K / kDepth<PAIR>;   // an even number; a slice's too
     const uint32_t begin = turns / 2 * t.slice / t.slices * 2, end = turns / 2 * (t.slice + 1) / t.slices * 2;
-    multiply<PAIR, F>(p + (uint64_t)t.i * T * PL * K, q + (uint64_t)t.j * T * PL * K, m.Mp - t.i * T, cols - t.j * T, K, begin, end - begin,
-                      reinterpret_cast<_Float16 *>(lds), acc);
+    constexpr bool kDown = OP == PRODUCT || OP == LAST;
+    multiply<PAIR, kDown, F>(p + (uint64_t)t.i * T * PL * K, kDown ? q : q + (uint64_t)t.j * T * PL * K, m.Mp - t.i * T, kDown ? t.j * T : cols - t.j * T,
+                             cols, K, begin, end - begin, reinterpret_cast<_Float16 *>(lds), acc);
     if (T > 64 && t.slices > 1) {
         // The last slice to come adds all of them up, in their order.  The sums pass the caches of the XCDs by (device-scope atomics of
         // 8 bytes; fences would write these caches back): they are where all see them once the wait is over, and counted after that.
@@ -352,7 +371,7 @@ __global__ __launch_bounds__(kThreads<F>, F == 128 ? 2 : 1) void k_ortho_product
     }
 
     float *fold = reinterpret_cast<float *>(lds) + (T == 64 ? 0 : w) * KW * 64 * kPitch, *own = fold + group * 64 * kPitch;
-    const bool turned = OP == PRODUCT || (OP == LAST && m.tall) || ((OP == GRAM || OP == SQUARE) && t.i != t.j);
+    const bool turned = (OP == LAST && m.tall) || ((OP == GRAM || OP == SQUARE) && t.i != t.j);
     const auto finish = [&](auto which) __attribute__((always_inline)) {
         constexpr int block = decltype(which)::value, BI = FI / kBlocks;
         if (block) __syncthreads();
@@ -452,7 +471,7 @@ __global__ __launch_bounds__(kThreads<F>, F == 128 ? 2 : 1) void k_ortho_product
                 const uint32_t both = (uint32_t)__builtin_bit_cast(uint16_t, h) | (uint32_t)__builtin_bit_cast(uint16_t, l) << 16;
                 at[e] = __builtin_bit_cast(float, both);
             }
-            _Float16 *dst = OP == GRAM ? a : OP == SQUARE ? b : x;
+            _Float16 *dst = OP == GRAM ? a : OP == SQUARE ? b : x_next;
             *reinterpret_cast<half8 *>(dst + to) = hi;
             if (PAIR || OP == PRODUCT) *reinterpret_cast<half8 *>(dst + to + (PAIR ? 16 : plane_x)) = lo;
         }
@@ -475,7 +494,7 @@ __global__ __launch_bounds__(kThreads<F>, F == 128 ? 2 : 1) void k_ortho_product
                 hi[e] = __builtin_bit_cast(_Float16, (uint16_t)both);
                 lo[e] = __builtin_bit_cast(_Float16, (uint16_t)(both >> 16));
             }
-            _Float16 *dst = OP == GRAM ? a : OP == SQUARE ? b : xt_next;
+            _Float16 *dst = OP == GRAM ? a : b;
             const uint64_t to = place<PAIR>(j0 + r, i0 + k, m.Mp);
             *reinterpret_cast<half8 *>(dst + to) = hi;
             if (PAIR) *reinterpret_cast<half8 *>(dst + to + 16) = lo;
@@ -512,7 +531,7 @@ static hipError_t iterate(const OrthoLayout &lay, const OrthoCall &c, hipStream_
     }
     for (uint32_t k = 0; k < c.steps; ++k) {
         const Polynomial f = {c.coefficients[3 * k], c.coefficients[3 * k + 1], c.coefficients[3 * k + 2]};
-        product<GRAM, PAIR>(lay, c, f, 0, s);
+        product<GRAM, PAIR>(lay, c, f, k & 1u, s);
         product<SQUARE, PAIR>(lay, c, f, 0, s);
         if (k + 1 < c.steps) product<PRODUCT, PAIR>(lay, c, f, k & 1u, s);
         else product<LAST, PAIR>(lay, c, f, k & 1u, s);

@@ -12,8 +12,7 @@ namespace co3 {
 // that the products have no edges.  Planes of fp16, in elements from the workspace's planes on; the low parts lie behind the high ones.
 struct MatDev {
     uint64_t offset, ld;        // in the caller's vector
-    uint64_t x;                 // X, hi and lo: [Mp][Np]
-    uint64_t xt;                // X^T twice, of one step and of the next: [Np][Mp]; hi, or hi and lo
+    uint64_t x;                 // X twice, of one step and of the next, hi and lo: [Mp][Np]
     uint64_t a, b;              // A = X X^T and B = b A + c A A: [Mp][Mp]; hi, or hi and lo
     uint32_t rows, cols;        // as the caller has it
     uint32_t M, N, Mp, Np;
