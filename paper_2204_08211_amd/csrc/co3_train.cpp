@@ -175,23 +175,33 @@ Tiles choose_tiles(const std::vector<MatDev> &mats, int op, bool pair)
     Tiles best;
     double least = 0.0;
     for (const Rate &rate : kRates) {
+        uint64_t count = 0;
+        uint32_t longest = 0;
+        for (const MatDev &m : mats) {
+            const uint64_t ni = (m.Mp + rate.tile - 1) / rate.tile, nj = (m.Np + rate.tile - 1) / rate.tile;
+            count += op == PRODUCT ? ni * nj : ni * (ni + 1) / 2;
+            longest = std::max(longest, turns_of(m, op, depth));
+        }
+        if (best.rate && count > 4 * (uint64_t)rate.room) continue;   // fills the chip with larger tiles as well
+        if (count > kMaxTiles) return {};
         const std::vector<TileDev> v = tiles_of(mats, op, rate.tile, depth);
         const size_t room = rate.room, whole = v.size() / room * room;
         double all = 0.0, behind = 0.0;
         for (size_t q = 0; q < v.size(); ++q) (q < whole ? all : behind) += turns_of(mats[v[q].mat], op, depth);
         all += behind;
         const auto consider = [&](size_t from, double share) {
+            if (from < v.size() && std::max(share, (double)kLeastTurns) * 1.5 > longest) return;   // nothing would be cut
             Tiles t = cut(mats, op, rate, depth, v, from, share);
             const double time = time_of(mats, op, depth, t);
             if (!best.rate || time < least) { least = time; best = std::move(t); }
         };
         consider(v.size(), 0.0);
-        if (v.size() > 16384) break;   // fills the chip either way
         consider(whole, behind / room);
+        if (v.size() > 4 * room) continue;
         for (double part : {1.0, 0.7, 0.5, 0.35, 0.25}) consider(0, part * all / room);
         uint32_t before = 0;   // no slice longer than a shorter matrix's whole sum
         for (const TileDev &t : v)
-            if (const uint32_t n = turns_of(mats[t.mat], op, depth); n != before && (before = n) != turns_of(mats[v[0].mat], op, depth)) consider(0, n);
+            if (const uint32_t n = turns_of(mats[t.mat], op, depth); n != before && (before = n) != longest) consider(0, n);
     }
     return best;
 }
@@ -240,7 +250,7 @@ int build_plan(uint32_t count, const co3_matrix *matrices, co3_matrix_plan *p)
     if (l.small) halves = diagonals = 0;
     const Tiles gram = choose_tiles(mats, GRAM, PL == 2), square = choose_tiles(mats, SQUARE, PL == 2), product = choose_tiles(mats, PRODUCT, PL == 2);
     for (const Tiles *t : {&gram, &square, &product}) {
-        if (t->v.size() > kMaxTiles) return CO3_ERR_CAPACITY;
+        if (!t->rate || t->v.size() > kMaxTiles) return CO3_ERR_CAPACITY;
         l.slices = std::max(l.slices, t->parts);
         l.slice_floats = std::max(l.slice_floats, (uint64_t)t->parts * t->rate->tile * t->rate->tile * t->rate->groups);
     }
