@@ -111,16 +111,37 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_layernorm(co3_layerno
 }
 
 // Slices that a user's rows are cut into, one workgroup each.  A slice leaves a row of partial sums for either gradient, 16
-// bytes a column written and read again, so it has at least 16 rows of three tensors.
-constexpr uint32_t kSliceRows = 16, kSlices = 512;
-static uint32_t backward_slices(uint32_t U, uint64_t rows)
+// bytes a column written and read again, so it has 16 rows of three tensors.  Long rows, which a workgroup takes one at a time, are cut
+// into slices of four while that leaves CUs without one (200 rows of 16000 bf16 elements, 13 or 50 slices: 75 or 37 us).
+static uint32_t backward_slices(uint32_t U, uint64_t rows, uint32_t cols)
 {
-    const uint64_t most = kSlices / U > 1 ? kSlices / U : 1;
-    const uint64_t n = (rows + kSliceRows - 1) / kSliceRows;
-    return (uint32_t)(n < 1 ? 1 : n < most ? n : most);
+    const auto slices = [&](uint64_t each, uint32_t in_all) {
+        const uint64_t most = in_all / U > 1 ? in_all / U : 1, n = (rows + each - 1) / each;
+        return (uint32_t)(n < 1 ? 1 : n < most ? n : most);
+    };
+    const uint32_t n = slices(16, 512);
+    return cols > 1024 && n * U < 256 ? slices(4, 256) : n;
 }
 
-template <typename T, int TPR, int CH>
+// Where a slice's sums of a user go: to its place, or to the gradients themselves where it is the only one.
+__device__ inline float *grad_place(const co3_layernorm_backward_args &a, uint32_t u, uint32_t slice, uint32_t slices, float *partial, bool bias)
+{
+    float *const grad = bias ? a.dbias : a.dweight;
+    return slices > 1 ? partial + (((uint64_t)u * slices + slice) * 2 + (bias ? 1 : 0)) * a.cols : grad ? grad + u * a.grad_stride : nullptr;
+}
+template <int V>
+__device__ inline void put_grad(float *to, int j, int cols, const float (&g)[V], bool add)
+{
+    if (!to) return;
+    typename Pack<float, V>::V v;
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = g[i];
+    if (add) v += load_pack<float, V>(to + j, cols - j);
+    store_pack<float, V>(to + j, cols - j, v);
+}
+
+// GRADS: the weight's gradients too, in registers while the slice's rows go by.
+template <typename T, int TPR, int CH, bool GRADS>
 __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_layernorm_backward(co3_layernorm_backward_args a, uint32_t slices, float *partial)
 {
     constexpr int V = kVec<T>, WG = TPR > 256 ? TPR : 256, ROWS = WG / TPR;
@@ -169,8 +190,8 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_layernorm_backward(co
                 const float xh = live && j + i < cols ? ((float)px[c][i] - mean) * rstd : 0.f;
                 s1 += t;
                 s2 += t * xh;
-                dw[c][i] += d * xh;
-                db[c][i] += d;
+                if (GRADS) dw[c][i] += d * xh;
+                if (GRADS) db[c][i] += d;
             }
         }
         row_sums<TPR>(s1, s2, lds[(k - r0) / ROWS % 2]);
@@ -195,7 +216,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_layernorm_backward(co
             store_pack<T, V>(dx + j, cols - j, p);
         }
     }
-    if (!a.dweight && !a.dbias) return;
+    if (!GRADS || (!a.dweight && !a.dbias)) return;
     if (ROWS > 1) {   // the workgroup's rows after one another
         for (int w = 0; w < ROWS; ++w) {
             if (sub == w) {
@@ -213,21 +234,40 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_layernorm_backward(co
         }
         if (sub != ROWS - 1) return;
     }
+    float *const to_w = grad_place(a, u, blockIdx.x, slices, partial, false), *const to_b = grad_place(a, u, blockIdx.x, slices, partial, true);
 #pragma unroll
-    for (int c = 0; c < CH; ++c)
+    for (int c = 0; c < CH; ++c) {
+        const int j = at + c * TPR * V;
+        put_grad<V>(to_w, j, cols, dw[c], slices == 1 && a.accumulate);
+        put_grad<V>(to_b, j, cols, db[c], slices == 1 && a.accumulate);
+    }
+}
+
+// The weight's gradients of rows that are too long for a workgroup's registers: a thread goes down a slice's rows in its columns.
+template <typename T>
+__global__ __launch_bounds__(256) void k_layernorm_columns(co3_layernorm_backward_args a, uint32_t slices, float *partial)
+{
+    constexpr int V = kVec<T>;
+    const uint32_t u = blockIdx.y;
+    const int cols = (int)a.cols, j = (int)(blockIdx.z * 256 + threadIdx.x) * V;
+    const uint64_t base = (uint64_t)u * a.rows_per_user;
+    const uint64_t r0 = base + a.rows_per_user * blockIdx.x / slices, r1 = base + a.rows_per_user * (blockIdx.x + 1) / slices;
+    float dw[V], db[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) dw[i] = db[i] = 0.f;
+#pragma unroll 4
+    for (uint64_t r = r0; r < r1; ++r) {
+        const auto x = load_pack<T, V>(static_cast<const T *>(a.x) + r * a.x_stride + j, cols - j);
+        const auto dy = load_pack<T, V>(static_cast<const T *>(a.dy) + r * a.dy_stride + j, cols - j);
+        const float mean = a.mean[r], rstd = a.rstd[r];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const int j = at + c * TPR * V + i;
-            if (j >= cols) continue;
-            if (slices > 1) {
-                float *p = partial + ((uint64_t)u * slices + blockIdx.x) * 2 * cols;
-                p[j] = dw[c][i];
-                p[cols + j] = db[c][i];
-            } else {
-                if (a.dweight) { float *p = a.dweight + u * a.grad_stride + j; *p = a.accumulate ? *p + dw[c][i] : dw[c][i]; }
-                if (a.dbias) { float *p = a.dbias + u * a.grad_stride + j; *p = a.accumulate ? *p + db[c][i] : db[c][i]; }
-            }
+            dw[i] += (float)dy[i] * (((float)x[i] - mean) * rstd);
+            db[i] += (float)dy[i];
         }
+    }
+    put_grad<V>(grad_place(a, u, blockIdx.x, slices, partial, false), j, cols, dw, slices == 1 && a.accumulate);
+    put_grad<V>(grad_place(a, u, blockIdx.x, slices, partial, true), j, cols, db, slices == 1 && a.accumulate);
 }
 
 // The slices' sums of a user, 64 columns of either gradient a workgroup: a wavefront takes every sixteenth slice.
@@ -265,7 +305,15 @@ template <typename T, int TPR, int CH>
 static void backward(const co3_layernorm_backward_args &a, uint32_t slices, float *partial, hipStream_t s)
 {
     constexpr int WG = TPR > 256 ? TPR : 256;
-    k_layernorm_backward<T, TPR, CH><<<dim3(slices, a.U), dim3(WG), WG > TPR ? 8 * a.cols : 0, s>>>(a, slices, partial);
+    if (TPR <= 512) {
+        k_layernorm_backward<T, TPR, CH, TPR <= 512><<<dim3(slices, a.U), dim3(WG), WG > TPR ? 8 * a.cols : 0, s>>>(a, slices, partial);
+        return;
+    }
+    if (a.dweight || a.dbias)   // first: dx may take the place of what they are made of
+        k_layernorm_columns<T><<<dim3(slices, a.U, (a.cols + 256 * kVec<T> - 1) / (256 * kVec<T>)), dim3(256), 0, s>>>(a, slices, partial);
+    const uint64_t most = a.U < 2048 ? 2048 / a.U : 1;
+    const uint32_t rows = (uint32_t)(a.rows_per_user < most ? a.rows_per_user : most);
+    if (rows) k_layernorm_backward<T, TPR, CH, TPR <= 512><<<dim3(rows, a.U), dim3(WG), 0, s>>>(a, rows, nullptr);
 }
 
 template <typename T>
@@ -304,7 +352,7 @@ static void backward_of(const co3_layernorm_backward_args &a, uint32_t slices, f
 
 size_t layernorm_backward_workspace_bytes(uint32_t U, uint64_t rows_per_user, uint32_t cols)
 {
-    const uint32_t slices = backward_slices(U, rows_per_user);
+    const uint32_t slices = backward_slices(U, rows_per_user, cols);
     return slices > 1 ? (size_t)U * slices * 2 * cols * sizeof(float) : 0;
 }
 
@@ -320,7 +368,7 @@ hipError_t launch_layernorm(const co3_layernorm_args &a, hipStream_t s)
 hipError_t launch_layernorm_backward(const co3_layernorm_backward_args &a, hipStream_t s)
 {
     const bool grads = a.dweight || a.dbias;
-    const uint32_t slices = backward_slices(a.U, a.rows_per_user);
+    const uint32_t slices = backward_slices(a.U, a.rows_per_user, a.cols);
     float *partial = static_cast<float *>(a.workspace);
     {
         ProfScope prof(K_LAYERNORM_BACKWARD, s);

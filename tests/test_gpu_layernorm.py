@@ -154,6 +154,26 @@ def test_rows_apart_at_any_element_and_in_place(cols, name):
     assert torch.equal(B.co3_layernorm(xx, weight, bias, y=xx)[0], B.co3_layernorm(x, weight, bias)[0])
 
 
+@pytest.mark.parametrize("name", ["float32", "bfloat16"])
+@pytest.mark.parametrize("rows", [9, 70])
+@pytest.mark.parametrize("cols", [700, 12000, 20000])
+def test_gradients_where_dx_takes_the_place_of_dy_or_x(cols, rows, name):
+    import torch
+    from paper_2204_08211_amd import binding as B
+    x = torch.randn(2, rows, cols, device="cuda:0").to(dtype_of(name))
+    dy = torch.randn(2, rows, cols, device="cuda:0").to(dtype_of(name))
+    _, mean, rstd = B.co3_layernorm(x)
+    want = [torch.empty(2, cols, device="cuda:0") for _ in range(2)]
+    dx = B.co3_layernorm_backward(dy, x, None, mean, rstd, dweight=want[0], dbias=want[1])
+    _, edw, edb = plain_backward(dy, x, None, mean, rstd)
+    assert float((want[0].double() - edw).abs().max()) <= 2.0 ** -18 * rows and float((want[1].double() - edb).abs().max()) <= 2.0 ** -18 * rows
+    for place in ("dy", "x"):
+        t = dict(dy=dy.clone(), x=x.clone())
+        got = [torch.empty(2, cols, device="cuda:0") for _ in range(2)]
+        B.co3_layernorm_backward(t["dy"], t["x"], None, mean, rstd, dx=t[place], dweight=got[0], dbias=got[1])
+        assert torch.equal(t[place], dx) and torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
 def test_rows_far_from_zero_constant_and_not_finite():
     import torch
     from paper_2204_08211_amd import binding as B
