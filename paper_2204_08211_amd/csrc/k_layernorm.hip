@@ -6,6 +6,9 @@
 // Both are bound by memory: every element is read once and written once, the row stays in registers in between.  All
 // sums are fp32 over a lane's elements and then over the lanes in a fixed order; the variance is the mean of the squared
 // distances from the mean, which a mean far larger than the spread does not harm.
+//
+// Measured (MI355X, a large copy runs at 4.8 TB/s): forward 16384 x 4096 bf16 58 us = 4.6 TB/s; backward 16384 x 8192 bf16 175 us =
+// 4.6 TB/s, eight users' 1024 x 1001 fp32 29 us = 3.4 TB/s (24 us, and 4 us for the sums of the slices).
 #include "co3_internal.h"
 #include "tensor_types.h"
 
@@ -56,6 +59,8 @@ __device__ inline void row_sums(float &v, float &u, float (*lds)[2])
     }
 }
 
+// A row stays in registers between its sums and its result.  Few lanes a row where rows are short, so that a load brings many of them; one
+// wavefront up to 512 packs, which needs no meeting; a workgroup beyond.
 template <typename T, int TPR, int CH>
 __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_layernorm(co3_layernorm_args a)
 {
@@ -140,7 +145,9 @@ __device__ inline void put_grad(float *to, int j, int cols, const float (&g)[V],
     store_pack<float, V>(to + j, cols - j, v);
 }
 
-// GRADS: the weight's gradients too, in registers while the slice's rows go by.
+// GRADS: the weight's gradients too, in registers while the slice's rows go by.  At most two workgroups of 256 threads fit a CU with
+// them (240 registers of 8192 bf16 columns), so xh and t are computed twice rather than kept: 249 us kept by workgroups of 512 threads, 209
+// us with the next row asked for ahead instead, 175 us so.
 template <typename T, int TPR, int CH, bool GRADS>
 __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_layernorm_backward(co3_layernorm_backward_args a, uint32_t slices, float *partial)
 {
@@ -243,7 +250,8 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_layernorm_backward(co
     }
 }
 
-// The weight's gradients of rows that are too long for a workgroup's registers: a thread goes down a slice's rows in its columns.
+// The weight's gradients of rows that are too long for a workgroup's registers: a thread goes down a slice's rows in its columns.  x and dy
+// are read twice then: 2000 x 32768 bf16 170 us, 395 us with gradients in registers that spill.
 template <typename T>
 __global__ __launch_bounds__(256) void k_layernorm_columns(co3_layernorm_backward_args a, uint32_t slices, float *partial)
 {
