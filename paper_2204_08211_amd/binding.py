@@ -527,13 +527,36 @@ MUON_COEFFICIENTS = (3.4445, -4.7750, 2.0315)
 
 
 @functools.lru_cache(maxsize=None)
+@functools.lru_cache(maxsize=1)
+def _tensor_types():
+    import torch
+    return {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+
+
 def tensor_type(dtype):
     """CO3_F32, CO3_BF16 or CO3_F16 of a torch dtype."""
-    import torch
-    types = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
-    if dtype not in types:
+    t = _tensor_types().get(dtype)
+    if t is None:
         raise TypeError(f"float32, bfloat16 or float16 tensors are taken, not {dtype}")
-    return types[dtype]
+    return t
+
+
+def _allocate_on(stream):
+    """For what a call allocates: memory of the stream that it runs on, which is not given to another before it is done there."""
+    import torch
+    return torch.cuda.stream(stream)   # None: the current one
+
+
+def _stream_of(gpu, stream):
+    """The stream of a call with tensors of this GPU (as Tensor.get_device() says it: -1 is the host)."""
+    if gpu < 0:
+        raise ValueError("tensors on a GPU are taken")
+    if _torch_c is None:
+        _stream()
+    on = _torch_c._cuda_getDevice() if stream is None else stream.device.index
+    if on != gpu:
+        raise ValueError(f"tensors on GPU {on}, which the stream is of, are taken, not on {gpu}")
+    return _torch_c._cuda_getCurrentRawStream(gpu) if stream is None else stream.cuda_stream
 
 
 class MatrixPlan:
@@ -558,6 +581,7 @@ class MatrixPlan:
         self.handle = h
         self.workspace_bytes = int(lib().co3_matrix_plan_workspace_bytes(h))
         self.elements = int(lib().co3_matrix_plan_elements(h))
+        self.gpu = torch.cuda.current_device()
 
     def close(self):
         if getattr(self, "handle", None):
@@ -585,14 +609,19 @@ def _ns_coefficients(coefficients, steps):
 
 
 def _matrix_vector(plan, t, name):
-    if t.dtype != plan.dtype or t.dim() != 1 or not t.is_contiguous() or t.numel() < plan.elements:
-        raise ValueError(f"{name}: a contiguous vector of at least {plan.elements} {plan.dtype} elements is taken")
+    if t.dtype != plan.dtype or t.dim() != 1 or not t.is_contiguous() or t.numel() < plan.elements or t.get_device() != plan.gpu:
+        raise ValueError(f"{name}: a contiguous vector of at least {plan.elements} {plan.dtype} elements on the plan's GPU is taken")
 
 
-def _matrix_workspace(plan, workspace, device):
+def _matrix_workspace(plan, workspace, status, stream):
+    if status is not None and (status.get_device() != plan.gpu or status.numel() < STATUS_WORDS or status.element_size() != 8):
+        raise ValueError(f"status: {STATUS_WORDS} int64 elements on the plan's GPU are taken")
     if workspace is None:
         import torch
-        workspace = torch.empty(plan.workspace_bytes, dtype=torch.uint8, device=device)
+        with _allocate_on(stream):
+            workspace = torch.empty(plan.workspace_bytes, dtype=torch.uint8, device=f"cuda:{plan.gpu}")
+    elif workspace.get_device() != plan.gpu:
+        raise ValueError("workspace: memory of the plan's GPU is taken")
     return workspace
 
 
@@ -601,16 +630,18 @@ def co3_orthogonalize(plan, g, out=None, steps=5, coefficients=MUON_COEFFICIENTS
     """out = scale * Newton-Schulz iterate of every matrix of the flat vector g (out may be g; None: a new vector, with
     zeros outside the matrices).  coefficients: (a, b, c) of every step, or `steps` triples.  status (int64
     [STATUS_WORDS], or None): matrices whose norm is not finite are added to status[STAT_NONFINITE]."""
+    _matrix_vector(plan, g, "g")
+    on = _stream_of(plan.gpu, stream)
     if out is None:
         import torch
-        out = torch.zeros_like(g)
-    _matrix_vector(plan, g, "g")
+        with _allocate_on(stream):
+            out = torch.zeros_like(g)
     _matrix_vector(plan, out, "out")
-    workspace = _matrix_workspace(plan, workspace, g.device)
+    workspace = _matrix_workspace(plan, workspace, status, stream)
     c = _ns_coefficients(coefficients, steps)
     a = _pack_orthogonalize(g.data_ptr(), out.data_ptr(), c.ctypes.data, int(steps), float(eps),
                           0 if status is None else status.data_ptr(), workspace.data_ptr(), workspace.numel())
-    _check("co3_orthogonalize", lib().co3_orthogonalize(plan.handle, a, _stream(stream)))
+    _check("co3_orthogonalize", lib().co3_orthogonalize(plan.handle, a, on))
     return out
 
 
@@ -620,20 +651,24 @@ def co3_muon_update(plan, g, momentum, model, eta, beta=0.95, nesterov=True, wei
     eta scale NS(u), for every matrix of the float32 vectors; the elements outside the matrices stay."""
     for t, name in ((g, "g"), (momentum, "momentum"), (model, "model")):
         _matrix_vector(plan, t, name)
-    workspace = _matrix_workspace(plan, workspace, g.device)
+    on = _stream_of(plan.gpu, stream)
+    workspace = _matrix_workspace(plan, workspace, status, stream)
     c = _ns_coefficients(coefficients, steps)
     a = _pack_muon(g.data_ptr(), momentum.data_ptr(), model.data_ptr(), c.ctypes.data, int(steps), float(eps), float(eta), float(beta),
                  float(weight_decay), int(bool(nesterov)), 0 if status is None else status.data_ptr(), workspace.data_ptr(),
                  workspace.numel())
-    _check("co3_muon_update", lib().co3_muon_update(plan.handle, a, _stream(stream)))
+    _check("co3_muon_update", lib().co3_muon_update(plan.handle, a, on))
 
 
 def _norm_rows(t, name):
     """(users, rows per user, columns, elements between rows) of a [rows, cols] or [users, rows, cols] tensor."""
     shape = t.shape
-    if len(shape) not in (2, 3):
+    if len(shape) == 3:
+        users, rows, cols = shape
+    elif len(shape) == 2:
+        users, (rows, cols) = 1, shape
+    else:
         raise ValueError(f"{name}: [rows, cols] or [users, rows, cols] is taken")
-    users, rows, cols = shape if len(shape) == 3 else (1, *shape)
     if t.is_contiguous():
         return users, rows, cols, cols
     stride = t.stride(-2) if rows > 1 else t.stride(0) if len(shape) == 3 and users > 1 else cols
@@ -644,11 +679,11 @@ def _norm_rows(t, name):
     return users, rows, cols, stride
 
 
-def _norm_vector(t, n, name):
+def _norm_vector(t, n, name, gpu, f32):
     if t is None:
         return 0
-    if t.dtype != _float32() or t.numel() != n or not t.is_contiguous():
-        raise ValueError(f"{name}: {n} contiguous float32 elements are taken")
+    if t.dtype is not f32 or t.numel() != n or t.get_device() != gpu or not t.is_contiguous():
+        raise ValueError(f"{name}: {n} contiguous float32 elements on x's device are taken")
     return t.data_ptr()
 
 
@@ -658,26 +693,29 @@ def _float32():
     return torch.float32
 
 
-def _rows_like(t, x, name):
+def _rows_like(t, shape, dtype, name, gpu):
     """Elements between the rows of a tensor of x's shape and type."""
-    if t.shape != x.shape or t.dtype != x.dtype:
-        raise ValueError(f"{name}: the shape and type of x are taken")
-    return x.shape[-1] if t.is_contiguous() else _norm_rows(t, name)[3]
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != gpu:
+        raise ValueError(f"{name}: the shape, type and device of x are taken")
+    return shape[-1] if t.is_contiguous() else _norm_rows(t, name)[3]
 
 
 def co3_layernorm(x, weight=None, bias=None, eps=1e-5, y=None, mean=None, rstd=None, stream=None):
     """(y, mean, rstd) of x [rows, cols] or [users, rows, cols] (float32, bfloat16, float16; rows may lie apart): y of x's
     type, mean and rstd float32 without the last dimension.  weight, bias: float32 [cols] or None.  y may be x."""
     users, rows, cols, stride = _norm_rows(x, "x")
+    shape, dtype, gpu, f32 = x.shape, x.dtype, x.get_device(), _float32()
+    kind = tensor_type(dtype)
     if y is None or mean is None or rstd is None:
         import torch
-        y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if y is None else y
-        mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if mean is None else mean
-        rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if rstd is None else rstd
-    a = _pack_layernorm(x.data_ptr(), y.data_ptr(), _norm_vector(weight, cols, "weight"), _norm_vector(bias, cols, "bias"),
-                      _norm_vector(mean, users * rows, "mean"), _norm_vector(rstd, users * rows, "rstd"), users * rows, stride,
-                      _rows_like(y, x, "y"), cols, tensor_type(x.dtype), float(eps), 0)
-    _check("co3_layernorm", lib().co3_layernorm(a, _stream(stream)))
+        with _allocate_on(stream):
+            y = torch.empty(shape, dtype=dtype, device=x.device) if y is None else y
+            mean = torch.empty(shape[:-1], dtype=f32, device=x.device) if mean is None else mean
+            rstd = torch.empty(shape[:-1], dtype=f32, device=x.device) if rstd is None else rstd
+    a = _pack_layernorm(x.data_ptr(), y.data_ptr(), _norm_vector(weight, cols, "weight", gpu, f32), _norm_vector(bias, cols, "bias", gpu, f32),
+                      _norm_vector(mean, users * rows, "mean", gpu, f32), _norm_vector(rstd, users * rows, "rstd", gpu, f32), users * rows, stride,
+                      _rows_like(y, shape, dtype, "y", gpu), cols, kind, float(eps), 0)
+    _check("co3_layernorm", lib().co3_layernorm(a, _stream_of(gpu, stream)))
     return y, mean, rstd
 
 
@@ -685,12 +723,12 @@ def co3_layernorm_backward_workspace_bytes(users, rows, cols):
     return int(lib().co3_layernorm_backward_workspace_bytes(int(users), int(rows), int(cols)))
 
 
-def _grad_rows(t, users, cols, name):
+def _grad_rows(t, users, cols, name, gpu, f32):
     """Elements between two users' gradients."""
     shape = t.shape
-    if t.dtype != _float32() or shape[-1] != cols or (shape[0] if len(shape) == 2 else 1) != users or len(shape) > 2 or \
-            (cols > 1 and t.stride(-1) != 1):
-        raise ValueError(f"{name}: float32 [users, cols] with contiguous rows is taken ([cols] for one user)")
+    if t.dtype is not f32 or t.get_device() != gpu or shape[-1] != cols or (shape[0] if len(shape) == 2 else 1) != users or \
+            len(shape) > 2 or (cols > 1 and t.stride(-1) != 1):
+        raise ValueError(f"{name}: float32 [users, cols] on x's device with contiguous rows is taken ([cols] for one user)")
     return t.stride(0) if users > 1 else cols
 
 
@@ -700,23 +738,28 @@ def co3_layernorm_backward(dy, x, weight, mean, rstd, dx=None, dweight=None, dbi
     the users' gradients that co3_encode reads) the weight's gradients of every user: written, or added with accumulate."""
     users, rows, cols, x_stride = _norm_rows(x, "x")
     stride = cols
+    shape, dtype, gpu, f32 = x.shape, x.dtype, x.get_device(), _float32()
+    kind = tensor_type(dtype)
     if dweight is not None:
-        stride = _grad_rows(dweight, users, cols, "dweight")
+        stride = _grad_rows(dweight, users, cols, "dweight", gpu, f32)
     if dbias is not None:
-        other = _grad_rows(dbias, users, cols, "dbias")
+        other = _grad_rows(dbias, users, cols, "dbias", gpu, f32)
         if dweight is not None and other != stride:
             raise ValueError("dweight and dbias: the same distance between users is taken")
         stride = other
     if dx is None or workspace is None:
         import torch
-        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if dx is None else dx
-        if workspace is None and (dweight is not None or dbias is not None):
-            workspace = torch.empty(co3_layernorm_backward_workspace_bytes(users, rows, cols), dtype=torch.uint8, device=x.device)
-    a = _pack_layernorm_backward(dy.data_ptr(), x.data_ptr(), dx.data_ptr(), _norm_vector(weight, cols, "weight"),
-                              _norm_vector(mean, users * rows, "mean"), _norm_vector(rstd, users * rows, "rstd"),
+        with _allocate_on(stream):
+            dx = torch.empty(shape, dtype=dtype, device=x.device) if dx is None else dx
+            if workspace is None and (dweight is not None or dbias is not None):
+                workspace = torch.empty(co3_layernorm_backward_workspace_bytes(users, rows, cols), dtype=torch.uint8, device=x.device)
+    if workspace is not None and workspace.get_device() != gpu:
+        raise ValueError("workspace: memory of x's GPU is taken")
+    a = _pack_layernorm_backward(dy.data_ptr(), x.data_ptr(), dx.data_ptr(), _norm_vector(weight, cols, "weight", gpu, f32),
+                              _norm_vector(mean, users * rows, "mean", gpu, f32), _norm_vector(rstd, users * rows, "rstd", gpu, f32),
                               0 if dweight is None else dweight.data_ptr(), 0 if dbias is None else dbias.data_ptr(),
-                              stride, rows, _rows_like(dy, x, "dy"), x_stride, _rows_like(dx, x, "dx"), users, cols,
-                              tensor_type(x.dtype), 1 if accumulate else 0, 0 if workspace is None else workspace.data_ptr(),
+                              stride, rows, _rows_like(dy, shape, dtype, "dy", gpu), x_stride, _rows_like(dx, shape, dtype, "dx", gpu), users, cols,
+                              kind, 1 if accumulate else 0, 0 if workspace is None else workspace.data_ptr(),
                               0 if workspace is None else workspace.numel())
-    _check("co3_layernorm_backward", lib().co3_layernorm_backward(a, _stream(stream)))
+    _check("co3_layernorm_backward", lib().co3_layernorm_backward(a, _stream_of(gpu, stream)))
     return dx

@@ -284,3 +284,29 @@ def test_another_stream_and_a_replayed_graph():
         torch.cuda.synchronize()
         for t, e in zip((y, mean, rstd, dx, grad), want):
             assert torch.equal(t, e)
+
+
+def test_stream_argument_and_refused_devices():
+    import torch
+    from paper_2204_08211_amd import binding as B
+    dev = "cuda:0"
+    x, dy = torch.randn(2, 700, 300, device=dev), torch.randn(2, 700, 300, device=dev)
+    w, grad, want_grad = torch.randn(300, device=dev), torch.zeros(2, 600, device=dev), torch.zeros(2, 600, device=dev)
+    want = B.co3_layernorm(x, w)
+    want_dx = B.co3_layernorm_backward(dy, x, w, *want[1:], dweight=want_grad[:, :300], dbias=want_grad[:, 300:])
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got = B.co3_layernorm(x, w, stream=side)
+    dx = B.co3_layernorm_backward(dy, x, w, *got[1:], dweight=grad[:, :300], dbias=grad[:, 300:], stream=side)
+    for _ in range(8):   # memory that a call let go of is not the current stream's to write
+        torch.full((B.co3_layernorm_backward_workspace_bytes(2, 700, 300),), 255, dtype=torch.uint8, device=dev)
+    torch.cuda.synchronize()
+    for t, e in zip((*got, dx, grad), (*want, want_dx, want_grad)):
+        assert torch.equal(t, e)
+    for bad in (dict(x=x.cpu()), dict(weight=w.cpu()), dict(y=torch.empty(2, 700, 300)), dict(mean=torch.empty(2, 700)), dict(x=x.cpu(), weight=w.cpu())):
+        with pytest.raises(ValueError):
+            B.co3_layernorm(**{"x": x, "weight": w, **bad})
+    for bad in (dict(dy=dy.cpu()), dict(mean=want[1].cpu()), dict(dx=torch.empty(2, 700, 300)), dict(dweight=torch.empty(2, 300)),
+                dict(workspace=torch.empty(1 << 20, dtype=torch.uint8))):
+        with pytest.raises(ValueError):
+            B.co3_layernorm_backward(**{"dy": dy, "x": x, "weight": w, "mean": want[1], "rstd": want[2], **bad})

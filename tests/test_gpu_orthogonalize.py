@@ -316,3 +316,29 @@ def test_another_stream_and_a_replayed_graph(shapes):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(m, em) and torch.equal(w, ew)
+
+
+def test_stream_argument_and_refused_devices():
+    import torch
+    from paper_2204_08211_amd import binding as B
+    dev = "cuda:0"
+    plan = B.MatrixPlan([(3, 50, 100), (6000, 200, 70)])
+    g = torch.randn(21000, device=dev)
+    want = B.co3_orthogonalize(plan, g)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    torch.cuda._sleep(50_000_000)   # the current stream is some milliseconds behind: what is made for the call is made on its stream
+    out = B.co3_orthogonalize(plan, g, stream=side)
+    torch.cuda.synchronize()
+    assert torch.equal(out, want)
+    with pytest.raises(ValueError):
+        B.co3_orthogonalize(plan, g.cpu())
+    with pytest.raises(ValueError):
+        B.co3_orthogonalize(plan, g, out=torch.empty(21000))
+    with pytest.raises(ValueError):
+        B.co3_orthogonalize(plan, g, workspace=torch.empty(plan.workspace_bytes, dtype=torch.uint8))
+    for status in (torch.zeros(8, dtype=torch.int64), torch.zeros(7, dtype=torch.int64, device=dev), torch.zeros(8, dtype=torch.int32, device=dev)):
+        with pytest.raises(ValueError):
+            B.co3_orthogonalize(plan, g, status=status)
+    with pytest.raises(ValueError):
+        B.co3_muon_update(plan, g, g.cpu(), g.clone(), eta=0.1)
