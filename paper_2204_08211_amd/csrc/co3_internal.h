@@ -171,7 +171,7 @@ namespace co3 {
 // Per-kernel event timing (profile.cpp).  A ProfScope around a launch records two events on
 // the stream when profiling is on, and does nothing otherwise.
 enum KernelId { K_ZERO = 0, K_QUANTIZE, K_REDUCE_HIST, K_BUILD_BOOKS, K_CHUNK_BITS, K_SCAN, K_PACK, K_DECODE, K_AGGREGATE, K_FUSED, K_MOMENTS, K_FIT, K_MODEL_WEIGHTS, K_MODEL_BIAS,
-                K_ORTHO_NORM, K_ORTHO_PACK, K_ORTHO_GRAM, K_ORTHO_SQUARE, K_ORTHO_PRODUCT, K_ORTHO_SMALL, K_LAYERNORM, K_LAYERNORM_BACKWARD, K_LAYERNORM_GRAD, K_COUNT };
+                K_ORTHO_NORM, K_ORTHO_PACK, K_ORTHO_GRAM, K_ORTHO_SQUARE, K_ORTHO_PRODUCT, K_ORTHO_SMALL, K_ORTHO_THIN, K_LAYERNORM, K_LAYERNORM_BACKWARD, K_LAYERNORM_GRAD, K_COUNT };
 bool profile_enabled();
 class ProfScope {
 public:

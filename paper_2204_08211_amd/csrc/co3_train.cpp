@@ -206,6 +206,22 @@ Tiles choose_tiles(const std::vector<MatDev> &mats, int op, bool pair)
     return best;
 }
 
+uint64_t gram_elements(const MatDev &m) { return m.M > 32 ? 64 * 64 : 32 * 32; }
+
+// Whether k_ortho_thin takes the matrices: while the parts of A that its workgroups read are few.  Its microseconds against those of the
+// products by tiles (fp32, five steps): 64 x 1024 56 : 117; 64 of these 163 : 184, 128 of them 305 : 250 (not taken); 64 x 8192 98 : 147,
+// 64 x 32768 244 : 267 (192 in bf16; not taken); 16 of 64 x 4096 189 : 178 (not taken); 32 x 32768 98 : 260; 512 of 16 x 512 303 : 388.
+bool thin(const std::vector<MatDev> &mats)
+{
+    double load = 0.0;
+    for (const MatDev &m : mats) {
+        const double strips = (m.N + kSmallN - 1) / kSmallN;
+        if (m.M > kSmallM) return false;
+        load += strips * (1.0 + strips / 64) * (double)(gram_elements(m) / 1024);
+    }
+    return load <= 2400.0;
+}
+
 int build_plan(uint32_t count, const co3_matrix *matrices, co3_matrix_plan *p)
 {
     OrthoLayout &l = p->lay;
@@ -247,10 +263,29 @@ int build_plan(uint32_t count, const co3_matrix *matrices, co3_matrix_plan *p)
     }
     l.small = 1;
     for (const MatDev &m : mats) l.small &= m.M <= kSmallM && m.N <= kSmallN;
-    if (l.small) halves = diagonals = 0;
-    const Tiles gram = choose_tiles(mats, GRAM, PL == 2), square = choose_tiles(mats, SQUARE, PL == 2), product = choose_tiles(mats, PRODUCT, PL == 2);
+    l.thin = !l.small && thin(mats);
+    Tiles gram, square, product;
+    if (l.small || l.thin) {
+        halves = diagonals = 0;
+    } else {
+        gram = choose_tiles(mats, GRAM, PL == 2);
+        square = choose_tiles(mats, SQUARE, PL == 2);
+        product = choose_tiles(mats, PRODUCT, PL == 2);
+        if (!gram.rate || !square.rate || !product.rate) return CO3_ERR_CAPACITY;
+    }
+    if (l.thin) {
+        pack.clear();
+        for (uint32_t k = 0; k < count; ++k) {
+            MatDev &m = mats[k];
+            const uint32_t strips = (m.N + kSmallN - 1) / kSmallN;
+            for (uint32_t j = 0; j < strips; ++j) pack.push_back({k, 0, (uint16_t)j, 0, 0, 1});
+            m.x = l.slice_floats; l.slice_floats += (uint64_t)strips * kSmallM * kSmallN;
+            m.a = l.slice_floats; l.slice_floats += (uint64_t)2 * strips * gram_elements(m);
+        }
+    }
     for (const Tiles *t : {&gram, &square, &product}) {
-        if (!t->rate || t->v.size() > kMaxTiles) return CO3_ERR_CAPACITY;
+        if (!t->rate) continue;
+        if (t->v.size() > kMaxTiles) return CO3_ERR_CAPACITY;
         l.slices = std::max(l.slices, t->parts);
         l.slice_floats = std::max(l.slice_floats, (uint64_t)t->parts * t->rate->tile * t->rate->tile * t->rate->groups);
     }
@@ -267,20 +302,20 @@ int build_plan(uint32_t count, const co3_matrix *matrices, co3_matrix_plan *p)
     if (hipMalloc(&p->tables, at[4]) != hipSuccess) return CO3_ERR_HIP;
     unsigned char *d = static_cast<unsigned char *>(p->tables);
     const auto copy = [&](size_t to, const auto &v) {
-        return hipMemcpy(d + to, v.data(), v.size() * sizeof(v[0]), hipMemcpyHostToDevice) == hipSuccess;
+        return v.empty() || hipMemcpy(d + to, v.data(), v.size() * sizeof(v[0]), hipMemcpyHostToDevice) == hipSuccess;
     };
     if (!copy(0, mats) || !copy(at_parts, parts)) return CO3_ERR_HIP;
     for (int k = 0; k < 4; ++k)
         if (!copy(at[k], *all[k])) return CO3_ERR_HIP;
     l.mats = reinterpret_cast<const MatDev *>(d);
     l.parts = reinterpret_cast<const PartDev *>(d + at_parts);
-    const auto launch = [&](int k, uint32_t form) {
-        return LaunchDev{reinterpret_cast<const TileDev *>(d + at[k]), (uint32_t)all[k]->size(), form};
+    const auto launch = [&](int k, const Rate *rate) {
+        return LaunchDev{reinterpret_cast<const TileDev *>(d + at[k]), (uint32_t)all[k]->size(), rate ? rate->form : 0u};
     };
-    l.pack = launch(0, 0);
-    l.gram = launch(1, gram.rate->form);
-    l.square = launch(2, square.rate->form);
-    l.product = launch(3, product.rate->form);
+    l.pack = launch(0, nullptr);
+    l.gram = launch(1, gram.rate);
+    l.square = launch(2, square.rate);
+    l.product = launch(3, product.rate);
     return CO3_OK;
 }
 

@@ -532,6 +532,7 @@ static hipError_t iterate(const OrthoLayout &lay, const OrthoCall &c, hipStream_
         ProfScope prof(K_ORTHO_NORM, s);
         k_ortho_norm<T, MUON><<<dim3(lay.nparts), dim3(256), 0, s>>>(lay, c);
     }
+    if (lay.thin) return launch_orthogonalize_thin(lay, c, s);
     {
         ProfScope prof(K_ORTHO_PACK, s);
         k_ortho_pack<T, MUON, PAIR><<<dim3(lay.pack.n), dim3(256), 0, s>>>(lay, c);

@@ -53,6 +53,7 @@ struct OrthoLayout {
     LaunchDev pack, gram, square, product;    // of X; of A's lower half; of B's lower half; of X
     uint32_t nmat, nparts;
     uint32_t small;                           // all matrices are: a workgroup takes one through all steps (k_ortho_small.hip)
+    uint32_t thin;                            // all have few rows: a workgroup takes 128 columns through a step (there too); pack: these strips
     uint32_t slices;                          // counters of slices, and places for their sums
     uint64_t slice_floats;                    // fp32 elements of these
     int32_t type, products;
@@ -77,6 +78,7 @@ struct OrthoCall {
 hipError_t launch_orthogonalize(const OrthoLayout &lay, const OrthoCall &c, hipStream_t s);
 constexpr uint32_t kSmallM = 64, kSmallN = 128;   // the largest X of launch_orthogonalize_small
 hipError_t launch_orthogonalize_small(const OrthoLayout &lay, const OrthoCall &c, hipStream_t s);
+hipError_t launch_orthogonalize_thin(const OrthoLayout &lay, const OrthoCall &c, hipStream_t s);   // behind the norms
 
 }  // namespace co3
 

@@ -10,7 +10,7 @@ namespace co3 {
 
 static const char *kKernelNames[K_COUNT] = {"k_zero_u64", "k_quantize", "k_reduce_hist", "k_build_books", "k_chunk_bits",
                                             "k_scan_chunks", "k_pack", "k_decode", "k_aggregate", "k_encode_fused", "k_moments", "k_fit_params",
-                                            "k_model_weights", "k_model_bias", "k_ortho_norm", "k_ortho_pack", "k_ortho_gram", "k_ortho_square", "k_ortho_product", "k_ortho_small",
+                                            "k_model_weights", "k_model_bias", "k_ortho_norm", "k_ortho_pack", "k_ortho_gram", "k_ortho_square", "k_ortho_product", "k_ortho_small", "k_ortho_thin",
                                             "k_layernorm", "k_layernorm_backward", "k_layernorm_grad"};
 
 struct ProfRecord { int kid; hipEvent_t a, b; };

@@ -342,3 +342,39 @@ def test_stream_argument_and_refused_devices():
             B.co3_orthogonalize(plan, g, status=status)
     with pytest.raises(ValueError):
         B.co3_muon_update(plan, g, g.cpu(), g.clone(), eta=0.1)
+
+
+# Matrices of up to 64 rows or columns, 128 of the others at a time: one, two and many such strips, the last one of a single column,
+# sums of 32 x 32 and 64 x 64, and just beyond what is taken that way (64 x 40000).
+FEW_ROWS = [[(64, 129)], [(1, 129), (129, 1), (33, 128), (128, 33)], [(32, 256), (256, 32), (2, 777), (64, 700), (5, 5)], [(17, 20000)], [(20000, 17)],
+            [(64, 8192), (31, 1000)], [(40, 300)] * 40, [(64, 40000)]]
+
+
+@pytest.mark.parametrize("name", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("shapes", FEW_ROWS)
+def test_few_rows(shapes, name):
+    import torch
+    dtype = getattr(torch, name)
+    check(shapes, dtype, noise, tolerance(dtype))
+    check(shapes, dtype, falling, tolerance(dtype))
+    for steps in (1, 2):
+        check(shapes[:5], dtype, noise, tolerance(dtype), steps=steps)
+
+
+@pytest.mark.parametrize("name", ["float32", "bfloat16"])
+def test_few_rows_with_one_dominant_direction(name):
+    test_one_dominant_direction((48, 900), name)
+
+
+def test_few_rows_zeros_and_values_that_are_not_finite():
+    for name in ("float32", "bfloat16"):
+        for bad in ((40, 300), (300, 20)):
+            test_zeros_and_values_that_are_not_finite(bad, name)
+
+
+def test_few_rows_coefficients_in_place_update_and_graph():
+    test_coefficients_of_their_own_for_every_step([(50, 260), (40, 60)])
+    test_matrices_side_by_side_and_in_place((50, 60, 300))
+    for nesterov in (True, False):
+        test_update([(64, 300), (1000, 10), (10, 64)], nesterov)
+    test_another_stream_and_a_replayed_graph([(33, 500), (300, 64)])
