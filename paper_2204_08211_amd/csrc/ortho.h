@@ -14,6 +14,7 @@ struct MatDev {
     uint64_t offset, ld;        // in the caller's vector
     uint64_t x;                 // X twice, of one step and of the next, hi and lo: [Mp][Np]
     uint64_t a, b;              // A = X X^T and B = b A + c A A: [Mp][Mp]; hi, or hi and lo
+                                // k_ortho_thin: x and a are fp32 elements of the workspace's sums, X by strips and, twice, the parts of A
     uint32_t rows, cols;        // as the caller has it
     uint32_t M, N, Mp, Np;
     uint32_t part, nparts;      // its partial sums of squares
