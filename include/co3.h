@@ -353,8 +353,9 @@ typedef struct co3_matrix_plan co3_matrix_plan;   /* layout of a set of matrices
 /* How the products of fp16 operands are formed (every sum is fp32).  An operand is a pair hi + lo of fp16
  * numbers, 22 bits.  CO3_PRODUCTS_PAIR multiplies hi hi + hi lo + lo hi: the results have about fp32's
  * precision.  CO3_PRODUCTS_HIGH multiplies the high parts only, at a third of the work: errors of about
- * 2e-3 of the result, the size of its rounding to bf16.  The iterate itself stays a pair either way, so that
- * what the steps amplify is not the rounding.                                                         */
+ * 2e-3 of the result, the size of its rounding to bf16, where it has some hundred elements, whose roundings average
+ * out; up to 1.5e-2 of a result of few elements.  The iterate itself stays a pair either way, so that what the
+ * steps amplify is not the rounding.                                                                  */
 enum { CO3_PRODUCTS_PAIR = 0, CO3_PRODUCTS_HIGH = 1 };
 
 /* count matrices of a vector of `type` (co3_muon_update takes CO3_F32).  Allocates small device tables;

@@ -561,14 +561,14 @@ def _stream_of(gpu, stream):
 
 class MatrixPlan:
     """co3_matrix_plan: matrices (offset, rows, cols[, ld]) of a flat vector of `dtype`, and the factor of each one's
-    orthogonalised form (scales; None: 1).  products None: PRODUCTS_HIGH for
-    bfloat16, PRODUCTS_PAIR for the other types, whose rounding is finer than that."""
+    orthogonalised form (scales; None: 1).  products: PRODUCTS_PAIR, about fp32's precision, or PRODUCTS_HIGH, a third of
+    the matrix instructions at errors of about bfloat16's rounding."""
 
-    def __init__(self, matrices, dtype=None, scales=None, products=None):
+    def __init__(self, matrices, dtype=None, scales=None, products=PRODUCTS_PAIR):
         import torch
         dtype = torch.float32 if dtype is None else dtype
         self.dtype, self.count = dtype, len(matrices)
-        self.products = (PRODUCTS_HIGH if dtype == torch.bfloat16 else PRODUCTS_PAIR) if products is None else int(products)
+        self.products = PRODUCTS_PAIR if products is None else int(products)
         scales = [1.0] * self.count if scales is None else [float(x) for x in scales]
         assert len(scales) == self.count
         table = (Matrix * self.count)()

@@ -11,8 +11,9 @@
 // (of 4096 x 25088 noise, X_0's entries are 1.6 on average).  Scales are powers of two: they round nothing.  X is a pair
 // hi + lo of 22 bits, since small singular values grow up to a^steps times (485 at five steps of Muon's a = 3.4445)
 // while large ones stay: the rounding of the iterate to 11 bits, spread over all directions, grows with them (a
-// matrix of one dominant direction and 10^-3 noise: 9e-2 off, with the pair 2e-4).  Roundings of A and B need no pair for
-// results of 16 bits: where the singular values are small, so are A and B beside a (2e-3 off, the size of bf16's own rounding).
+// matrix of one dominant direction and 10^-3 noise: 9e-2 off, with the pair 2e-4).  The operands of the products are pairs too, unless the
+// caller asks for their high parts alone: where the singular values are small, so are A and B beside a, and their roundings do not
+// grow (2e-3 off, the size of bf16's own rounding; a few elements, whose roundings do not average out, up to 1.5e-2).
 //
 // Measured (MI355X; a large copy runs at 4.8 TB/s, the library's fp16 product of 4096 x 4096 at 1.37 PFLOP/s in 100 us):
 // one product B X of 4096 x 4096, high parts, 140 us = 0.98 PFLOP/s, of which 120 us are the sums; 1.14 PFLOP/s of 4096 x 25088 in

@@ -1,0 +1,51 @@
+"""How far orthogonalised matrices are from the iteration in 64 bits, in every form (pytest -m gpu): a workgroup's, a launch a step, tiles.
+
+Tolerances, of the difference's 2-norm over the result's.  A result y + e, where e is what the iteration is off, is rounded to the
+nearest number of the type: that is no further from y + e than y's own rounding is + |e|, so it is off by at most y's rounding + 2 |e|.
+Pairs leave |e| <= 2^-17, as derived in test_gpu_orthogonalize.py for six steps.  High parts are rounded by 2^-11 at most and 2^-12 in the mean;
+a step takes that up to six times, from its three factors.  Over hundreds of elements the roundings come to their mean, three such steps long:
+2^-8.  Those of a few elements need not: 6 2^-11 a step, five steps long, 2^-6, and twice that as small directions grow."""
+import pytest
+
+from test_gpu_orthogonalize import falling, lay_out, noise, rel, steps_of
+
+pytestmark = pytest.mark.gpu
+
+FORMS = {"a workgroup": [(64, 64), (33, 100), (128, 64), (1, 5)], "a launch a step": [(64, 1024), (700, 40), (1, 777)],
+         "tiles": [(1000, 2048), (257, 1023), (33, 4097), (1, 777)], "large tiles": [(2304, 2304)]}
+
+
+def results(shapes, dtype, make, **plan_args):
+    """(result, the iteration in 64 bits) of every matrix, with the plan's own choice of products unless one is given."""
+    import torch
+    from paper_2204_08211_amd import binding as B
+    matrices, n = lay_out(shapes)
+    g = torch.zeros(n, device="cuda:0", dtype=dtype)
+    for k, (at, rows, cols) in enumerate(matrices):
+        g[at:at + rows * cols] = make(k, rows, cols).reshape(-1).to(dtype)
+    out = B.co3_orthogonalize(B.MatrixPlan(matrices, dtype=dtype, **plan_args), g)
+    for at, rows, cols in matrices:
+        s = slice(at, at + rows * cols)
+        yield out[s].view(rows, cols), steps_of(g[s].view(rows, cols))
+
+
+@pytest.mark.parametrize("name", ["bfloat16", "float16"])
+@pytest.mark.parametrize("what", sorted(FORMS))
+def test_results_of_16_bits_are_rounded_once(what, name):
+    import torch
+    dtype = getattr(torch, name)
+    for make in (noise, falling):
+        for out, want in results(FORMS[what], dtype, make):
+            assert rel(out, want) <= rel(want.to(dtype), want) + 2 * 2.0 ** -17, tuple(out.shape)
+
+
+@pytest.mark.parametrize("name", ["float32", "bfloat16"])
+@pytest.mark.parametrize("what", sorted(FORMS))
+def test_high_parts_alone_on_request(what, name):
+    import torch
+    from paper_2204_08211_amd import binding as B
+    dtype = getattr(torch, name)
+    for make in (noise, falling):
+        for out, want in results(FORMS[what], dtype, make, products=B.PRODUCTS_HIGH):
+            off = 2.0 ** -8 if out.numel() >= 256 else 2.0 ** -5
+            assert rel(out, want) <= (off if name == "float32" else rel(want.to(dtype), want) + 2 * off), tuple(out.shape)
