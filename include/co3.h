@@ -410,7 +410,8 @@ int co3_muon_update(const co3_matrix_plan *plan, const co3_muon_args *args, void
 /* Layer norm over rows of `cols` elements:  mean, var (of the row, biased), rstd = 1 / sqrt(var + eps),
  * y = (x - mean) rstd weight + bias.  weight and bias (fp32 [cols], a layer's part of the flat model) may each
  * be NULL (1 and 0), mean and rstd (fp32 [rows], for the backward pass) too.  Rows and y's rows lie x_stride and
- * y_stride elements apart (>= cols).  All pointers are aligned as their elements are; y may be x.             */
+ * y_stride elements apart (>= cols).  All pointers are aligned as their elements are; y may be x.  The stream's and
+ * the tensors' GPU is the current one, here and in the backward pass.                                         */
 typedef struct {
     const void *x;
     void *y;

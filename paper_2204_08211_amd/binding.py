@@ -559,6 +559,15 @@ def _stream_of(gpu, stream):
     return _torch_c._cuda_getCurrentRawStream(gpu) if stream is None else stream.cuda_stream
 
 
+def _call_on(gpu, call, *args):
+    """call(*args) with this GPU current: the handle of a GPU's default stream is 0, which means that of the current one."""
+    if _torch_c._cuda_getDevice() == gpu:
+        return call(*args)
+    import torch
+    with torch.cuda.device(gpu):
+        return call(*args)
+
+
 class MatrixPlan:
     """co3_matrix_plan: matrices (offset, rows, cols[, ld]) of a flat vector of `dtype`, and the factor of each one's
     orthogonalised form (scales; None: 1).  products: PRODUCTS_PAIR, about fp32's precision, or PRODUCTS_HIGH, a third of
@@ -715,7 +724,8 @@ def co3_layernorm(x, weight=None, bias=None, eps=1e-5, y=None, mean=None, rstd=N
     a = _pack_layernorm(x.data_ptr(), y.data_ptr(), _norm_vector(weight, cols, "weight", gpu, f32), _norm_vector(bias, cols, "bias", gpu, f32),
                       _norm_vector(mean, users * rows, "mean", gpu, f32), _norm_vector(rstd, users * rows, "rstd", gpu, f32), users * rows, stride,
                       _rows_like(y, shape, dtype, "y", gpu), cols, kind, float(eps), 0)
-    _check("co3_layernorm", lib().co3_layernorm(a, _stream_of(gpu, stream)))
+    on = _stream_of(gpu, stream)
+    _check("co3_layernorm", _call_on(gpu, lib().co3_layernorm, a, on))
     return y, mean, rstd
 
 
@@ -761,5 +771,6 @@ def co3_layernorm_backward(dy, x, weight, mean, rstd, dx=None, dweight=None, dbi
                               stride, rows, _rows_like(dy, shape, dtype, "dy", gpu), x_stride, _rows_like(dx, shape, dtype, "dx", gpu), users, cols,
                               kind, 1 if accumulate else 0, 0 if workspace is None else workspace.data_ptr(),
                               0 if workspace is None else workspace.numel())
-    _check("co3_layernorm_backward", lib().co3_layernorm_backward(a, _stream_of(gpu, stream)))
+    on = _stream_of(gpu, stream)
+    _check("co3_layernorm_backward", _call_on(gpu, lib().co3_layernorm_backward, a, on))
     return dx
