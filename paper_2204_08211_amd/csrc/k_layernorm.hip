@@ -302,11 +302,21 @@ __global__ __launch_bounds__(1024) void k_layernorm_grad(co3_layernorm_backward_
     *out = a.accumulate ? *out + s : s;
 }
 
+// A launch of HIP has fewer than 2^32 threads: rows beyond that (2^22 by 1024 threads each, 2^29 by eight) have launches of their own.
 template <typename T, int TPR, int CH>
 static void forward(const co3_layernorm_args &a, hipStream_t s)
 {
     constexpr int WG = TPR > 256 ? TPR : 256, ROWS = WG / TPR;
-    k_layernorm<T, TPR, CH><<<dim3((uint32_t)((a.rows + ROWS - 1) / ROWS)), dim3(WG), 0, s>>>(a);
+    constexpr uint64_t most = ((1ull << 32) - 1) / WG * ROWS;
+    for (uint64_t row = 0; row < a.rows; row += most) {
+        co3_layernorm_args part = a;
+        part.rows = a.rows - row < most ? a.rows - row : most;
+        part.x = static_cast<const T *>(a.x) + row * a.x_stride;
+        part.y = static_cast<T *>(a.y) + row * a.y_stride;
+        if (a.mean) part.mean = a.mean + row;
+        if (a.rstd) part.rstd = a.rstd + row;
+        k_layernorm<T, TPR, CH><<<dim3((uint32_t)((part.rows + ROWS - 1) / ROWS)), dim3(WG), 0, s>>>(part);
+    }
 }
 
 template <typename T, int TPR, int CH>
