@@ -74,10 +74,10 @@ bool stays_bounded(uint32_t steps, const float *coef)
     for (uint32_t k = 0; k < steps; ++k) {
         const double a = coef[3 * k], b = coef[3 * k + 1], c = coef[3 * k + 2];
         if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) return false;
-        double at[4] = {top * top, -b / (2 * c), 0.0, 0.0};
-        const double root = std::sqrt(9 * b * b - 20 * a * c);   // NaN, and infinities for c = 0, are no place between the ends
-        at[2] = c != 0.0 ? (-3 * b + root) / (10 * c) : -a / (3 * b);
-        at[3] = (-3 * b - root) / (10 * c);
+        // p' = 0: one root by the sum of -3 b and the square root that does not cancel, the other from the roots' product a / (5 c), which
+        // is -a / (3 b) where c is 0.  NaN and infinities are no place between the ends.
+        const double sum = -3 * b - std::copysign(std::sqrt(9 * b * b - 20 * a * c), b);
+        const double at[4] = {top * top, -b / (2 * c), sum / (10 * c), 2 * a / sum};
         double most = 0.0, factor = 0.0;
         for (double t : at) {
             if (!(t > 0.0 && t <= top * top)) continue;
