@@ -118,14 +118,20 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_layernorm(co3_layerno
 // Slices that a user's rows are cut into, one workgroup each.  A slice leaves a row of partial sums for either gradient, 16
 // bytes a column written and read again, so it has 16 rows of three tensors.  Long rows, which a workgroup takes one at a time, are cut
 // into slices of four while that leaves CUs without one (200 rows of 16000 bf16 elements, 13 or 50 slices: 75 or 37 us).
+// However many there are, a slice's fp32 accumulators take 512 rows at most: 8192 terms of one sign have left a sum 1.2e-4 off.
+constexpr uint32_t kMostTerms = 512;
 static uint32_t backward_slices(uint32_t U, uint64_t rows, uint32_t cols)
 {
     const auto slices = [&](uint64_t each, uint32_t in_all) {
         const uint64_t most = in_all / U > 1 ? in_all / U : 1, n = (rows + each - 1) / each;
         return (uint32_t)(n < 1 ? 1 : n < most ? n : most);
     };
-    const uint32_t n = slices(16, 512);
-    return cols > 1024 && n * U < 256 ? slices(4, 256) : n;
+    uint32_t n = slices(16, 512);
+    if (cols > 1024 && n * U < 256) n = slices(4, 256);
+    // rows of a workgroup at a time, each with accumulators of its own: of fp32 elements, and no fewer of 16 bits
+    const uint32_t at_once = cols <= 32 ? 32 : cols <= 64 ? 16 : cols <= 128 ? 8 : cols <= 1024 ? 4 : 1;
+    const uint64_t least = (rows + kMostTerms * at_once - 1) / (kMostTerms * at_once);
+    return n < least ? (uint32_t)least : n;
 }
 
 // Where a slice's sums of a user go: to its place, or to the gradients themselves where it is the only one.
@@ -278,28 +284,29 @@ __global__ __launch_bounds__(256) void k_layernorm_columns(co3_layernorm_backwar
     put_grad<V>(grad_place(a, u, blockIdx.x, slices, partial, true), j, cols, db, slices == 1 && a.accumulate);
 }
 
-// The slices' sums of a user, 64 columns of either gradient a workgroup: a wavefront takes every sixteenth slice.
+// The slices' sums of a user, 64 columns of either gradient a workgroup: a wavefront takes every sixteenth slice.  In fp64, since there
+// may be thousands of slices.
 __global__ __launch_bounds__(1024) void k_layernorm_grad(co3_layernorm_backward_args a, uint32_t slices, const float *partial)
 {
-    __shared__ float part[16][64];
+    __shared__ double part[16][64];
     const uint32_t u = blockIdx.y, lane = threadIdx.x & 63u, w = threadIdx.x >> 6;
     const uint64_t c = (uint64_t)blockIdx.x * 64 + lane, cols = a.cols;   // dweight's columns, then dbias's
-    float s = 0.f;
+    double s = 0.0;
     if (c < 2 * cols) {
         const float *p = partial + (uint64_t)u * slices * 2 * cols + c;
 #pragma unroll 8
-        for (uint32_t k = w; k < slices; k += 16) s += p[k * 2 * cols];
+        for (uint32_t k = w; k < slices; k += 16) s += (double)p[k * 2 * cols];
     }
     part[w][lane] = s;
     __syncthreads();
     if (w || c >= 2 * cols) return;
-    s = 0.f;
+    s = 0.0;
 #pragma unroll
     for (int k = 0; k < 16; ++k) s += part[k][lane];
     float *out = c < cols ? a.dweight : a.dbias;
     if (!out) return;
     out += u * a.grad_stride + (c < cols ? c : c - cols);
-    *out = a.accumulate ? *out + s : s;
+    *out = (float)(a.accumulate ? (double)*out + s : s);
 }
 
 // A launch of HIP has fewer than 2^32 threads: rows beyond that (2^22 by 1024 threads each, 2^29 by eight) have launches of their own.

@@ -64,3 +64,12 @@ def test_backward_launches_fit(host, cols, kind):
                                         workspace=1 << 20, workspace_bytes=1 << 50)
             for grid, block, _ in launches(host.backward_launches, a):
                 assert all(0 < g and g * b < 1 << 32 for g, b in zip(grid, block)) and max(grid[1:]) <= 65535
+
+
+@pytest.mark.parametrize("cols", COLS + [32, 65, 128, 1024])
+def test_an_accumulator_takes_512_rows_at_most(host, cols):
+    at_once = 32 if cols <= 32 else 16 if cols <= 64 else 8 if cols <= 128 else 4 if cols <= 1024 else 1   # with accumulators of their own
+    for users in (1, 2, 16, 256, 257, 300, 65535):
+        for rows in (1, 512, 513, 8192, 32768, 100003, (1 << 31) // users - 1):
+            slices = max(1, host.backward_workspace(users, rows, cols) // (users * 2 * cols * 4))
+            assert -(-rows // slices) <= 512 * at_once
