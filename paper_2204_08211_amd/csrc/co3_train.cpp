@@ -37,14 +37,37 @@ constexpr uint64_t kMaxTiles = (1ull << 31) - 1;
 
 inline uint64_t end_of(const co3_matrix &m) { return m.offset + (uint64_t)(m.rows - 1) * m.ld + m.cols; }
 
-// Whether two matrices, a from b's first element or earlier on, share no element for certain: one ends before the other begins, or
-// their rows lie side by side at the same distance.
-bool apart(const co3_matrix &a, const co3_matrix &b)
+// The sum of floor((a i + b) / m) over i < n, modulo 2^64; a, b < 2^41, m <= 2^40, n <= 2^20.
+uint64_t sum_of_floors(uint64_t n, uint64_t m, uint64_t a, uint64_t b)
 {
-    if (end_of(a) <= b.offset) return true;
-    if (a.ld != b.ld) return false;
-    const uint64_t col = (b.offset - a.offset) % a.ld;   // b's first column in a's rows
-    return col >= a.cols && col + b.cols <= a.ld;
+    uint64_t sum = 0;
+    while (true) {   // as a greatest common divisor is found: the points below a line, counted by rows or by columns
+        sum += n * (n - 1) / 2 * (a / m) + n * (b / m);
+        a %= m;
+        b %= m;
+        const uint64_t top = a * n + b;
+        if (top < m) return sum;
+        n = top / m;
+        b = top % m;
+        std::swap(a, m);
+    }
+}
+
+// Whether two matrices share an element: a row of a begins less than a's columns before a row of b, or within it.
+bool meet(const co3_matrix &a, const co3_matrix &b)
+{
+    const int64_t offset = (int64_t)b.offset, last = offset + (int64_t)((b.rows - 1) * b.ld), wide = a.cols;
+    const auto first = [&](int64_t at) {   // the first row of a that begins there or behind it
+        const int64_t ahead = at - (int64_t)a.offset;
+        return ahead <= 0 ? 0 : std::min<uint64_t>(a.rows, ((uint64_t)ahead + a.ld - 1) / a.ld);
+    };
+    const uint64_t from = first(offset), to = first(last);
+    if (first(offset - wide + 1) < from || to < first(last + b.cols)) return true;   // by b's first row, in b's last row
+    // In between: rows that begin at q = q0 + a.ld i from b's first element on, with (q + wide - 1) mod b.ld < wide + b.cols - 1.
+    const uint64_t n = to - from, near = (uint64_t)wide + b.cols - 1;
+    if (n == 0 || near >= b.ld) return n != 0;
+    const uint64_t q = (a.offset + from * a.ld - b.offset + wide - 1) % b.ld, by = a.ld % b.ld;
+    return n + sum_of_floors(n, b.ld, by, q) - sum_of_floors(n, b.ld, by, q + b.ld - near) != 0;
 }
 
 int check_matrices(uint32_t count, const co3_matrix *m)
@@ -60,7 +83,7 @@ int check_matrices(uint32_t count, const co3_matrix *m)
     for (uint32_t k : order) {
         open.erase(std::remove_if(open.begin(), open.end(), [&](uint32_t o) { return end_of(m[o]) <= m[k].offset; }), open.end());
         for (uint32_t o : open)
-            if (!apart(m[o], m[k])) return CO3_ERR_ARG;
+            if (meet(m[o], m[k])) return CO3_ERR_ARG;
         open.push_back(k);
     }
     return CO3_OK;

@@ -71,3 +71,50 @@ def test_coefficients_are_taken_by_what_their_polynomials_reach(host):
             continue   # nearer to a limit than the grid is fine
         assert orthogonalize(host, plan, c) == (B.OK if most < 2 and factor < 7 else B.ERR_ARG), (c, most, factor)
     host.co3_matrix_plan_destroy(plan)
+
+
+def elements(matrices):
+    """Every matrix's elements, as a set each."""
+    return [{offset + r * ld + c for r in range(rows) for c in range(cols)} for offset, ld, rows, cols in matrices]
+
+
+def taken(host, matrices):
+    plan, rc = plan_of(host, matrices)
+    assert rc in (B.OK, B.ERR_ARG) and (rc == B.OK) == bool(plan.value)
+    host.co3_matrix_plan_destroy(plan)
+    return rc == B.OK
+
+
+@pytest.mark.parametrize("matrices,there", [
+    ([(0, 20, 10, 5), (10, 5, 1, 5)], True),                # a single row in another's gap, whatever its ld
+    ([(0, 20, 10, 5), (10, 5, 2, 5)], True),
+    ([(0, 20, 10, 5), (10, 5, 3, 5)], False),               # its third row is the other's second
+    ([(0, 16, 8, 8), (8, 32, 4, 8)], True),                 # every second gap
+    ([(0, 16, 8, 8), (8, 24, 4, 8)], False),
+    ([(0, 16, 8, 8), (8, 17, 8, 8)], False),
+    ([(0, 16, 1 << 20, 8), (8, 48, 1 << 18, 8)], True),
+    ([(0, 16, 1 << 20, 8), (8, 48, 1 << 18, 9)], False),
+    ([(0, 16, 1 << 20, 8), (8, 16 * ((1 << 20) - 2) + 1, 2, 8)], False),   # its last row ends in the other's last
+    ([(0, 16, 1 << 20, 8), (8, 16 * ((1 << 20) - 2) + 1, 2, 7)], True),
+    ([(5, (1 << 40) - 1, 1 << 20, 3), (0, 1 << 40, 3, 4)], False),         # one element nearer a row
+    ([(5, (1 << 40) - 1, 1 << 20, 3), (0, 1 << 40, 2, 4)], True),
+])
+def test_matrices_in_each_others_gaps(host, matrices, there):
+    assert taken(host, matrices) == there
+    assert taken(host, matrices[::-1]) == there
+
+
+def test_overlaps_against_sets_of_elements(host):
+    rng = np.random.default_rng(7)
+    seen = [0, 0]
+    for _ in range(3000):
+        matrices = []
+        for _ in range(rng.integers(2, 5)):
+            rows, cols = int(rng.integers(1, 9)), int(rng.integers(1, 7))
+            ld = cols + int(rng.choice([0, rng.integers(0, 40), 12 - cols if cols < 12 else 0, 24 - cols]))
+            matrices.append((int(rng.integers(0, 120)), ld, rows, cols))
+        every = elements(matrices)
+        apart = sum(map(len, every)) == len(set().union(*every))
+        assert taken(host, matrices) == apart, matrices
+        seen[apart] += 1
+    assert min(seen) > 200
