@@ -2,8 +2,11 @@
 #include <algorithm>
 #include <cmath>
 #include <functional>
+#include <iterator>
+#include <map>
 #include <new>
 #include <queue>
+#include <utility>
 #include <vector>
 
 #include "co3_internal.h"
@@ -77,14 +80,40 @@ int check_matrices(uint32_t count, const co3_matrix *m)
             return CO3_ERR_ARG;
         if (m[k].ld > (1ull << 40) || m[k].offset > (1ull << 60)) return CO3_ERR_ARG;   // the last element's index fits 64 bits
     }
-    std::vector<uint32_t> order(count), open;
+    // In the order of their first elements, each against those that have not ended there.  Matrices of the same ld are apart where their
+    // columns are: every ld has its open ones' columns, one or two pieces each, in order, and ended ones leave as they are met.
+    struct Lane {
+        std::map<uint64_t, std::pair<uint64_t, uint64_t>> pieces;   // from a column up to another, until that element
+        std::vector<uint32_t> open;
+    };
+    std::map<uint64_t, Lane> lanes;
+    std::vector<uint32_t> order(count);
     for (uint32_t k = 0; k < count; ++k) order[k] = k;
     std::sort(order.begin(), order.end(), [&](uint32_t a, uint32_t b) { return m[a].offset < m[b].offset; });
     for (uint32_t k : order) {
-        open.erase(std::remove_if(open.begin(), open.end(), [&](uint32_t o) { return end_of(m[o]) <= m[k].offset; }), open.end());
-        for (uint32_t o : open)
-            if (meet(m[o], m[k])) return CO3_ERR_ARG;
-        open.push_back(k);
+        const co3_matrix &c = m[k];
+        for (auto at = lanes.begin(); at != lanes.end();) {
+            std::vector<uint32_t> &open = at->second.open;
+            if (at->first == c.ld) { ++at; continue; }
+            open.erase(std::remove_if(open.begin(), open.end(), [&](uint32_t o) { return end_of(m[o]) <= c.offset; }), open.end());
+            for (uint32_t o : open)
+                if (meet(m[o], c)) return CO3_ERR_ARG;
+            at = open.empty() ? lanes.erase(at) : std::next(at);
+        }
+        Lane &lane = lanes[c.ld];
+        const uint64_t col = c.offset % c.ld, end = col + c.cols;
+        const std::pair<uint64_t, uint64_t> pieces[2] = {{col, std::min(end, c.ld)}, {0, end > c.ld ? end - c.ld : 0}};
+        for (const auto &[from, to] : pieces) {
+            if (from == to) continue;
+            auto at = lane.pieces.lower_bound(from);
+            if (at != lane.pieces.begin() && std::prev(at)->second.first > from) --at;
+            while (at != lane.pieces.end() && at->first < to) {
+                if (at->second.second > c.offset) return CO3_ERR_ARG;
+                at = lane.pieces.erase(at);
+            }
+            lane.pieces[from] = {to, end_of(c)};
+        }
+        lane.open.push_back(k);
     }
     return CO3_OK;
 }

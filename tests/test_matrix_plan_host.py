@@ -3,6 +3,7 @@ nothing (CPU only)."""
 import ctypes as C
 import os
 import subprocess
+import time
 
 import numpy as np
 import pytest
@@ -118,3 +119,16 @@ def test_overlaps_against_sets_of_elements(host):
         assert taken(host, matrices) == apart, matrices
         seen[apart] += 1
     assert min(seen) > 200
+
+
+def test_many_matrices_side_by_side(host):
+    """65536 columns of one row distance, and half as many beside rows of their own: in the order of n log n steps, far below a second
+    (every pair looked at takes several)."""
+    n = 65536
+    for matrices in ([(k, n, 4, 1) for k in range(n)], [(2 * k, n, 4, 1) for k in range(n // 2)] + [(4 * n + k, 1, 1, 1) for k in range(n // 2)]):
+        for there in (True, False):
+            if not there:
+                matrices = matrices[:-1] + [matrices[7]]
+            begin = time.process_time()
+            assert taken(host, matrices) == there
+            assert time.process_time() - begin < 1.5
