@@ -298,7 +298,8 @@ int build_plan(uint32_t count, const co3_matrix *matrices, co3_matrix_plan *p)
         m.a = halves; halves += PL * plane_a;
         m.b = halves; halves += PL * plane_a;
         p->elements = std::max(p->elements, end_of(c));
-        // parts of about 16384 elements, but at most 512 of a matrix: every workgroup that lays X out adds them up
+        // parts of about 16384 elements, but at most 512 of a matrix, and 1024 where a line is more than half of one: every workgroup that lays
+        // X out adds them up
         const uint64_t n = (uint64_t)c.rows * c.cols, want = std::max<uint64_t>(16384, (n + 511) / 512 + 7 & ~7ull);
         const bool whole = c.ld == c.cols;
         const uint64_t lines = whole ? 1 : c.rows, len = whole ? n : c.cols;
