@@ -159,11 +159,15 @@ __device__ inline int exchanged(int row, int chunk) { return chunk ^ (row >> 2 &
 
 // 64 lanes' 16 bytes from memory to LDS, without a register in between: from base + offset (of every lane) + k, to `lds` + 16 lane.
 // Written out, since the compiler would wait for all loads to LDS before every read of LDS.  Who reads waits with wait_loads().
+// m0 is named for the compiler's own writes to it; no value lives there, which is what its warning is about.
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ inline void load_to_lds(u32x4 base, uint32_t offset, uint32_t k, uint32_t lds)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" : : "s"(lds), "v"(offset), "s"(base), "s"(k) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" : : "s"(lds), "v"(offset), "s"(base), "s"(k) : "m0", "memory");
 }
+#pragma clang diagnostic pop
 // Until all but the wavefront's last `left` loads are there.
 template <int left>
 __device__ inline void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" : : "n"(left) : "memory"); }
@@ -303,7 +307,8 @@ __device__ __forceinline__ void multiply(const _Float16 *p, const _Float16 *q, u
     __syncthreads();
 }
 
-// Whether the workgroup is the last of a sum's slices to come, after its stores.
+// Whether the workgroup is the last of a sum's slices to come, after its stores.  The order of these and of the count is the hardware's, not
+// the language's: stores and loads of device scope pass the XCDs' caches by, so what the wait has seen done is where the last one's loads look.
 __device__ inline bool last_slice(uint32_t *counter, uint32_t slices, uint32_t *arrived)
 {
     wait_loads<0>();   // and stores
