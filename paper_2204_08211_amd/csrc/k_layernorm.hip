@@ -341,6 +341,8 @@ static void backward(const co3_layernorm_backward_args &a, uint32_t slices, floa
     if (rows) k_layernorm_backward<T, TPR, CH, TPR <= 512><<<dim3(rows, a.U), dim3(WG), 0, s>>>(a, rows, nullptr);
 }
 
+template <typename T> constexpr uint32_t kMostPacks = CO3_MAX_NORM_COLS / kVec<T>;   // of a row: 4096 of 16 bits, 8192 of fp32
+
 template <typename T>
 static void forward_of(const co3_layernorm_args &a, hipStream_t s)
 {
@@ -355,7 +357,7 @@ static void forward_of(const co3_layernorm_args &a, hipStream_t s)
     else if (packs <= 1024) forward<T, 256, 4>(a, s);
     else if (packs <= 2048) forward<T, 256, 8>(a, s);
     else if (packs <= 4096) forward<T, 1024, 4>(a, s);
-    else forward<T, 1024, 8>(a, s);
+    else if constexpr (kMostPacks<T> > 4096) forward<T, 1024, 8>(a, s);
 }
 
 template <typename T>
@@ -372,7 +374,7 @@ static void backward_of(const co3_layernorm_backward_args &a, uint32_t slices, f
     else if (packs <= 1024) backward<T, 256, 4>(a, slices, partial, s);
     else if (packs <= 2048) backward<T, 512, 4>(a, slices, partial, s);
     else if (packs <= 4096) backward<T, 1024, 4>(a, slices, partial, s);
-    else backward<T, 1024, 8>(a, slices, partial, s);
+    else if constexpr (kMostPacks<T> > 4096) backward<T, 1024, 8>(a, slices, partial, s);   // 128 registers, and 30 that spill
 }
 
 size_t layernorm_backward_workspace_bytes(uint32_t U, uint64_t rows_per_user, uint32_t cols)

@@ -1,6 +1,8 @@
 // Layer norm's host side for the CPU: what it would launch is written down instead.
 #include <string.h>
 
+#include <map>
+#include <string>
 #include <vector>
 
 #include "k_layernorm.hip"
@@ -13,6 +15,11 @@ struct Launch {
 std::vector<Launch> launches;
 dim3 next_grid, next_block;
 size_t bytes;   // of the kernels' first argument
+std::map<const void *, std::string> &kernels()   // those not launched yet; made before any other object here
+{
+    static std::map<const void *, std::string> m;
+    return m;
+}
 }  // namespace
 
 // What the compiler makes of a launch.
@@ -20,7 +27,10 @@ extern "C" {
 char __hip_fatbin[1];
 void **__hipRegisterFatBinary(const void *) { return nullptr; }
 void __hipUnregisterFatBinary(void **) {}
-void __hipRegisterFunction(void **, const void *, char *, const char *, unsigned, uint3 *, uint3 *, dim3 *, dim3 *, int *) {}
+void __hipRegisterFunction(void **, const void *kernel, char *, const char *name, unsigned, uint3 *, uint3 *, dim3 *, dim3 *, int *)
+{
+    kernels()[kernel] = name;
+}
 hipError_t __hipPushCallConfiguration(dim3 grid, dim3 block, size_t, hipStream_t)
 {
     next_grid = grid;
@@ -35,13 +45,16 @@ hipError_t __hipPopCallConfiguration(dim3 *grid, dim3 *block, size_t *lds, hipSt
     *stream = nullptr;
     return hipSuccess;
 }
-hipError_t hipLaunchKernel(const void *, dim3 grid, dim3 block, void **args, size_t, hipStream_t)
+hipError_t hipLaunchKernel(const void *kernel, dim3 grid, dim3 block, void **args, size_t, hipStream_t)
 {
     Launch l = {{grid.x, grid.y, grid.z}, {block.x, block.y, block.z}, {}};
     memcpy(l.args, args[0], bytes);
     launches.push_back(l);
+    kernels().erase(kernel);
     return hipSuccess;
 }
+uint32_t not_launched() { return (uint32_t)kernels().size(); }
+const char *one_not_launched() { return kernels().begin()->second.c_str(); }
 hipError_t hipGetLastError() { return hipSuccess; }
 
 // The launches of a call, at most `room` of them: their sizes, and the kernels' first arguments one behind the other.

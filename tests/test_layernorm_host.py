@@ -24,6 +24,7 @@ def host(tmp_path_factory):
                     "-o", str(so)] + flags, check=True)
     L = C.CDLL(str(so))
     L.backward_workspace.argtypes, L.backward_workspace.restype = [C.c_uint32, C.c_uint64, C.c_uint32], C.c_size_t
+    L.one_not_launched.restype = C.c_char_p
     return L
 
 
@@ -54,14 +55,18 @@ def test_forward_launches_fit_and_have_every_row_once(host, cols, kind):
         assert at == rows
 
 
+def backward_args(users, rows, cols, kind, grad):
+    return B.LayernormBackwardArgs(dy=1 << 20, x=1 << 30, dx=1 << 35, weight=None, mean=1 << 20, rstd=1 << 20, dweight=grad, dbias=grad, grad_stride=cols,
+                                   rows_per_user=rows, dy_stride=cols, x_stride=cols, dx_stride=cols, U=users, cols=cols, type=kind, accumulate=0,
+                                   workspace=1 << 20, workspace_bytes=1 << 50)
+
+
 @pytest.mark.parametrize("kind", [B.F32, B.BF16])
 @pytest.mark.parametrize("cols", COLS)
 def test_backward_launches_fit(host, cols, kind):
     for users, rows in ((1, 0), (1, 1), (3, 70001), (300, 1 << 20), (65535, 1), (65535, 32768), (1, (1 << 31) - 1)):
         for grad in (None, 1 << 40):
-            a = B.LayernormBackwardArgs(dy=1 << 20, x=1 << 30, dx=1 << 35, weight=None, mean=1 << 20, rstd=1 << 20, dweight=grad, dbias=grad, grad_stride=cols,
-                                        rows_per_user=rows, dy_stride=cols, x_stride=cols, dx_stride=cols, U=users, cols=cols, type=kind, accumulate=0,
-                                        workspace=1 << 20, workspace_bytes=1 << 50)
+            a = backward_args(users, rows, cols, kind, grad)
             for grid, block, _ in launches(host.backward_launches, a):
                 assert all(0 < g and g * b < 1 << 32 for g, b in zip(grid, block)) and max(grid[1:]) <= 65535
 
@@ -73,3 +78,11 @@ def test_an_accumulator_takes_512_rows_at_most(host, cols):
         for rows in (1, 512, 513, 8192, 32768, 100003, (1 << 31) // users - 1):
             slices = max(1, host.backward_workspace(users, rows, cols) // (users * 2 * cols * 4))
             assert -(-rows // slices) <= 512 * at_once
+
+
+def test_every_kernel_is_launched_by_some_call(host):
+    for kind in (B.F32, B.BF16, B.F16):
+        for cols in [1 << k for k in range(16)]:
+            launches(host.forward_launches, B.LayernormArgs(x=1 << 20, y=1 << 50, rows=9, x_stride=cols, y_stride=cols, cols=cols, type=kind, eps=1e-5))
+            launches(host.backward_launches, backward_args(2, 900, cols, kind, 1 << 40))
+    assert host.not_launched() == 0, host.one_not_launched().decode()
