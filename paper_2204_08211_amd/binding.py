@@ -623,14 +623,15 @@ def _matrix_vector(plan, t, name):
 
 
 def _matrix_workspace(plan, workspace, status, stream):
-    if status is not None and (status.get_device() != plan.gpu or status.numel() < STATUS_WORDS or status.element_size() != 8):
-        raise ValueError(f"status: {STATUS_WORDS} int64 elements on the plan's GPU are taken")
+    if status is not None and (status.get_device() != plan.gpu or status.numel() < STATUS_WORDS or status.element_size() != 8 or
+                               not status.is_contiguous()):
+        raise ValueError(f"status: {STATUS_WORDS} contiguous int64 elements on the plan's GPU are taken")
     if workspace is None:
         import torch
         with _allocate_on(stream):
             workspace = torch.empty(plan.workspace_bytes, dtype=torch.uint8, device=f"cuda:{plan.gpu}")
-    elif workspace.get_device() != plan.gpu:
-        raise ValueError("workspace: memory of the plan's GPU is taken")
+    elif workspace.get_device() != plan.gpu or not workspace.is_contiguous():
+        raise ValueError("workspace: contiguous memory of the plan's GPU is taken")
     return workspace
 
 
@@ -649,7 +650,7 @@ def co3_orthogonalize(plan, g, out=None, steps=5, coefficients=MUON_COEFFICIENTS
     workspace = _matrix_workspace(plan, workspace, status, stream)
     c = _ns_coefficients(coefficients, steps)
     a = _pack_orthogonalize(g.data_ptr(), out.data_ptr(), c.ctypes.data, int(steps), float(eps),
-                          0 if status is None else status.data_ptr(), workspace.data_ptr(), workspace.numel())
+                          0 if status is None else status.data_ptr(), workspace.data_ptr(), workspace.nbytes)
     _check("co3_orthogonalize", lib().co3_orthogonalize(plan.handle, a, on))
     return out
 
@@ -665,7 +666,7 @@ def co3_muon_update(plan, g, momentum, model, eta, beta=0.95, nesterov=True, wei
     c = _ns_coefficients(coefficients, steps)
     a = _pack_muon(g.data_ptr(), momentum.data_ptr(), model.data_ptr(), c.ctypes.data, int(steps), float(eps), float(eta), float(beta),
                  float(weight_decay), int(bool(nesterov)), 0 if status is None else status.data_ptr(), workspace.data_ptr(),
-                 workspace.numel())
+                 workspace.nbytes)
     _check("co3_muon_update", lib().co3_muon_update(plan.handle, a, on))
 
 
@@ -763,14 +764,14 @@ def co3_layernorm_backward(dy, x, weight, mean, rstd, dx=None, dweight=None, dbi
             dx = torch.empty(shape, dtype=dtype, device=x.device) if dx is None else dx
             if workspace is None and (dweight is not None or dbias is not None):
                 workspace = torch.empty(co3_layernorm_backward_workspace_bytes(users, rows, cols), dtype=torch.uint8, device=x.device)
-    if workspace is not None and workspace.get_device() != gpu:
-        raise ValueError("workspace: memory of x's GPU is taken")
+    if workspace is not None and (workspace.get_device() != gpu or not workspace.is_contiguous()):
+        raise ValueError("workspace: contiguous memory of x's GPU is taken")
     a = _pack_layernorm_backward(dy.data_ptr(), x.data_ptr(), dx.data_ptr(), _norm_vector(weight, cols, "weight", gpu, f32),
                               _norm_vector(mean, users * rows, "mean", gpu, f32), _norm_vector(rstd, users * rows, "rstd", gpu, f32),
                               0 if dweight is None else dweight.data_ptr(), 0 if dbias is None else dbias.data_ptr(),
                               stride, rows, _rows_like(dy, shape, dtype, "dy", gpu), x_stride, _rows_like(dx, shape, dtype, "dx", gpu), users, cols,
                               kind, 1 if accumulate else 0, 0 if workspace is None else workspace.data_ptr(),
-                              0 if workspace is None else workspace.numel())
+                              0 if workspace is None else workspace.nbytes)
     on = _stream_of(gpu, stream)
     _check("co3_layernorm_backward", _call_on(gpu, lib().co3_layernorm_backward, a, on))
     return dx

@@ -75,3 +75,60 @@ def test_layernorm_on_the_current_gpu(state):
     calls(None)
     calls(Stream(1, 0))
     assert state.calls == [(1, 101)] * 2 + [(1, 0)] * 2
+
+
+class Library(State):
+    """Takes what it is given, and keeps the argument structures."""
+
+    def __init__(self):
+        super().__init__()
+        self.current, self.kept = 1, []
+
+    def co3_layernorm_backward(self, args, stream):
+        self.kept.append(B.LayernormBackwardArgs.from_buffer_copy(args))
+        return B.OK
+
+    def co3_orthogonalize(self, plan, args, stream):
+        self.kept.append(B.OrthogonalizeArgs.from_buffer_copy(args))
+        return B.OK
+
+    def co3_matrix_plan_destroy(self, plan):
+        pass
+
+
+@pytest.fixture
+def library(monkeypatch):
+    s = Library()
+    monkeypatch.setattr(B, "_torch_c", s)
+    monkeypatch.setattr(B, "lib", lambda: s)
+    return s
+
+
+def with_workspace(workspace, status=None):
+    x, row, grad = (torch.zeros(*shape).as_subclass(OnGpu1) for shape in ((4, 8), (4,), (8,)))
+    B.co3_layernorm_backward(x, x, None, row, row, dx=x, dweight=grad, workspace=workspace)
+    plan = B.MatrixPlan.__new__(B.MatrixPlan)
+    plan.handle, plan.gpu, plan.dtype, plan.elements, plan.workspace_bytes = 1, 1, torch.float32, 32, 4096
+    g = torch.zeros(32).as_subclass(OnGpu1)
+    B.co3_orthogonalize(plan, g, g, workspace=workspace, status=status)
+
+
+def test_a_workspace_counts_its_bytes(library):
+    for dtype, size in ((torch.uint8, 1), (torch.float32, 4), (torch.int64, 8)):
+        with_workspace(torch.zeros(100, dtype=dtype).as_subclass(OnGpu1))
+        assert [a.workspace_bytes for a in library.kept[-2:]] == [100 * size] * 2
+
+
+def test_memory_that_is_not_there_is_refused(library):
+    """A tensor that is expanded, or has gaps, does not have the memory that its elements stand for."""
+    ok = torch.zeros(4096, dtype=torch.uint8)
+    for bad in (torch.zeros(1, dtype=torch.uint8).expand(4096), ok[::2]):
+        with pytest.raises(ValueError):
+            with_workspace(bad.as_subclass(OnGpu1))
+        plan = B.MatrixPlan.__new__(B.MatrixPlan)
+        plan.handle, plan.gpu, plan.dtype, plan.elements, plan.workspace_bytes = 1, 1, torch.float32, 32, 4096
+        with pytest.raises(ValueError):
+            B.co3_orthogonalize(plan, torch.zeros(32).as_subclass(OnGpu1), workspace=bad.as_subclass(OnGpu1))
+    for bad in (torch.zeros(1, dtype=torch.int64).expand(B.STATUS_WORDS), torch.zeros(2 * B.STATUS_WORDS, dtype=torch.int64)[::2]):
+        with pytest.raises(ValueError):
+            with_workspace(ok.as_subclass(OnGpu1), bad.as_subclass(OnGpu1))
