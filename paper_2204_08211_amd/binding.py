@@ -526,7 +526,6 @@ MAX_NORM_COLS = 32768
 MUON_COEFFICIENTS = (3.4445, -4.7750, 2.0315)
 
 
-@functools.lru_cache(maxsize=None)
 @functools.lru_cache(maxsize=1)
 def _tensor_types():
     import torch
