@@ -49,3 +49,15 @@ def test_high_parts_alone_on_request(what, name):
         for out, want in results(FORMS[what], dtype, make, products=B.PRODUCTS_HIGH):
             off = 2.0 ** -8 if out.numel() >= 256 else 2.0 ** -5
             assert rel(out, want) <= (off if name == "float32" else rel(want.to(dtype), want) + 2 * off), tuple(out.shape)
+
+
+@pytest.mark.parametrize("what", sorted(FORMS))
+def test_pairs_keep_their_bits(what):
+    """fp32 results of hundreds of elements and more.  A pair is rounded by 2^-22 at most and about 2^-24 in the root mean square; five such
+    roundings a step (X, A, B, and the products of low parts that two sums leave out), each taken up to 2.8 times, five steps long, come to
+    sqrt(25) 2.8 2^-24 = 2^-20.2 where they are independent: 2^-19.  Three bits less in any of them would be past it."""
+    import torch
+    for make in (noise, falling):
+        for out, want in results(FORMS[what], torch.float32, make):
+            if out.numel() >= 256:
+                assert rel(out, want) <= 2.0 ** -19, tuple(out.shape)
