@@ -339,7 +339,8 @@ int co3_ps_aggregate(const co3_plan *plan, const co3_aggregate_args *args, void 
 enum { CO3_F32 = 0, CO3_BF16 = 1, CO3_F16 = 2 };
 
 /* Matrices of the flat vector: row r, column c of a matrix is element offset + r ld + c.  They may
- * lie at any offset and in any order, side by side in the same rows too, and must not overlap.    */
+ * lie at any offset and in any order, side by side in the same rows too, and in each other's gaps
+ * at another distance; no two may share an element.                                               */
 typedef struct {
     uint64_t offset;
     uint64_t ld;             /* elements between rows, >= cols                                 */
@@ -361,10 +362,13 @@ enum { CO3_PRODUCTS_PAIR = 0, CO3_PRODUCTS_HIGH = 1 };
 /* count matrices of a vector of `type` (co3_muon_update takes CO3_F32).  Allocates small device tables;
  * synchronises the device.  Errors: CO3_ERR_ARG for a null pointer, no matrices or more than 65536, a size, an
  * ld, a scale, a type or products outside the above, matrices that overlap; CO3_ERR_CAPACITY where the host's
- * memory, or the 2^31 - 1 tiles of a launch, do not suffice.                                            */
+ * memory, or the 2^32 threads of a launch, do not suffice.                                              */
 int co3_matrix_plan_create(uint32_t count, const co3_matrix *matrices, int32_t type, int32_t products,
                            co3_matrix_plan **out);
 void co3_matrix_plan_destroy(co3_matrix_plan *plan);
+/* Next to nothing for sets within 64 x 128 each; up to 512 bytes a column for sets of few rows (the longer side's elements are the
+ * columns); otherwise, a matrix, 8 bytes times the product of its sides rounded up to multiples of 64, and 8 (from high parts
+ * 4) times the square of the shorter: a matrix of one row beside larger ones has 512 bytes an element.      */
 size_t co3_matrix_plan_workspace_bytes(const co3_matrix_plan *plan);
 uint64_t co3_matrix_plan_elements(const co3_matrix_plan *plan);   /* the vector's least length   */
 

@@ -36,7 +36,8 @@ inline size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 inline bool valid_type(int32_t t) { return t == CO3_F32 || t == CO3_BF16 || t == CO3_F16; }
 
 constexpr uint32_t kMaxMatrices = 65536, kMaxSide = 1u << 20;
-constexpr uint64_t kMaxTiles = (1ull << 31) - 1;
+constexpr uint64_t kMostThreads = (1ull << 32) - 1;   // of a launch: workgroups of 1024 threads at most for tiles, of 256 for norms and layout
+constexpr uint64_t kMaxTiles = kMostThreads / 1024, kMaxParts = kMostThreads / 256;
 
 inline uint64_t end_of(const co3_matrix &m) { return m.offset + (uint64_t)(m.rows - 1) * m.ld + m.cols; }
 
@@ -262,7 +263,7 @@ uint64_t gram_elements(const MatDev &m) { return m.M > 32 ? 64 * 64 : 32 * 32; }
 
 // Whether k_ortho_thin takes the matrices: while the parts of A that its workgroups read are few.  Its microseconds against those of the
 // products by tiles (fp32, five steps): 64 x 1024 56 : 117; 64 of these 163 : 184, 128 of them 305 : 250 (not taken); 64 x 8192 98 : 147,
-// 64 x 32768 244 : 267 (192 in bf16; not taken); 16 of 64 x 4096 189 : 178 (not taken); 32 x 32768 98 : 260; 512 of 16 x 512 303 : 388.
+// 64 x 32768 244 : 267 (192 from high parts; not taken); 16 of 64 x 4096 189 : 178 (not taken); 32 x 32768 98 : 260; 512 of 16 x 512 303 : 388.
 bool thin(const std::vector<MatDev> &mats)
 {
     double load = 0.0;
@@ -309,10 +310,10 @@ int build_plan(uint32_t count, const co3_matrix *matrices, co3_matrix_plan *p)
             for (uint64_t at = 0; at < len; at += piece)
                 parts.push_back({k, (uint32_t)std::min(group, lines - r), r * c.ld + at, std::min(piece, len - at)});
         m.nparts = (uint32_t)parts.size() - m.part;
-        if (parts.size() > kMaxTiles) return CO3_ERR_CAPACITY;
+        if (parts.size() > kMaxParts) return CO3_ERR_CAPACITY;
+        if (pack.size() + plane_x / (kBlock * kBlock) > kMaxParts) return CO3_ERR_CAPACITY;
         for (uint32_t i = 0; i < m.Mp / kBlock; ++i)
             for (uint32_t j = 0; j < m.Np / kBlock; ++j) pack.push_back({k, (uint16_t)i, (uint16_t)j, 0, 0, 1});
-        if (pack.size() > kMaxTiles) return CO3_ERR_CAPACITY;
     }
     l.small = 1;
     for (const MatDev &m : mats) l.small &= m.M <= kSmallM && m.N <= kSmallN;

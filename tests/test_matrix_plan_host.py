@@ -132,3 +132,13 @@ def test_many_matrices_side_by_side(host):
             begin = time.process_time()
             assert taken(host, matrices) == there
             assert time.process_time() - begin < 1.5
+
+
+def test_plans_beyond_what_a_launch_takes_are_refused(host):
+    """A launch has fewer than 2^32 threads: 2^24 workgroups of 256 lay matrices out by blocks of 64 x 64."""
+    plan, rc = plan_of(host, [(0, 1 << 17, 1 << 20, 1 << 17)])
+    host.co3_matrix_plan_destroy(plan)
+    assert rc == B.ERR_CAPACITY
+    plan, rc = plan_of(host, [(0, 1 << 13, 1 << 18, 1 << 13)])
+    host.co3_matrix_plan_destroy(plan)
+    assert rc == B.OK
