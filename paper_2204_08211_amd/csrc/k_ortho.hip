@@ -16,10 +16,10 @@
 // grow (2e-3 off, the size of bf16's own rounding; a few elements, whose roundings do not average out, up to 1.5e-2).
 //
 // Measured (MI355X; a large copy runs at 4.8 TB/s, the library's fp16 product of 4096 x 4096 at 1.37 PFLOP/s in 100 us):
-// one product B X of 4096 x 4096, high parts, 140 us = 0.98 PFLOP/s, of which 120 us are the sums; 1.14 PFLOP/s of 4096 x 25088 in
-// pairs.  The chip lowers its clock to 1.5 GHz under it: with no loads and no reads of LDS at all the same matrix instructions take
-// 94 us.  A product of a few hundred tiles is bound by what a CU gets from the caches (12 to 25 us, whatever the tile), then
-// by launches of 3 us.  Norm and layout are bound by memory.
+// one product B X of 4096 x 4096 in pairs 345 us = 1.19 PFLOP/s, of 4096 x 25088 1.14; from high parts alone 140 us = 0.98 PFLOP/s, of which
+// 120 us are the sums.  The chip lowers its clock to 1.5 GHz under it: with no loads and no reads of LDS at all the same matrix
+// instructions take 94 us.  A product of a few hundred tiles (10 to 30 us) is bound by what a CU gets from the caches, whatever the tile, and by
+// what comes before its first turn and behind its last: first loads, the old X, the split, the stores.  Norm and layout are bound by memory.
 #include <type_traits>
 
 #include "co3_internal.h"

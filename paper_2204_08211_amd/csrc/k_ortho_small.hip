@@ -6,7 +6,7 @@
 // A and B are symmetric: a lane's four rows of a column are written as four columns of a row.
 //
 // Bound by the chain of its phases: three products a step, each with LDS reads, some hundred vector instructions a wavefront and a
-// meeting of the workgroup behind it.  64 x 64 from high parts 1.8 us a step, 64 x 128 in pairs 3.6 us, and 8 us for the launch, the norm
+// meeting of the workgroup behind it.  64 x 64 in pairs 2.4 us a step (from high parts 1.8), 64 x 128 3.6 us, and 8 us for the launch, the norm
 // and the ends (the seventeen launches of k_ortho.hip: 70 to 80 us).
 //
 // Matrices of as few rows and more columns (k_ortho_thin): a workgroup has 128 columns, a launch is a step.  Five steps of 64 x 1024 fp32

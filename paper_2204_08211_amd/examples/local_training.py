@@ -138,7 +138,7 @@ def main():
     a = p.parse_args()
     net = Network(a.width, a.hidden, a.blocks, a.outputs)
     errors, bits = train(net, a.users, a.rows, a.iters, a.eta, sgd=a.sgd)
-    print(f"U={a.users} d={net.d} {'plain updates' if a.sgd else 'orthogonalised updates'}: mean squared error "
+    print(f"U={a.users} d={net.d} {'orthogonalised updates' if a.sgd is None else 'plain updates'}: mean squared error "
           + ", ".join(f"{errors[t]:.4f} at {t}" for t in sorted({0, a.iters // 4, a.iters // 2, a.iters - 1})) + f"; {bits:.3f} bit/element")
 
 
