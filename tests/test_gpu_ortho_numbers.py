@@ -7,7 +7,7 @@ a step takes that up to six times, from its three factors.  Over hundreds of ele
 2^-8.  Those of a few elements need not: 6 2^-11 a step, five steps long, 2^-6, and twice that as small directions grow."""
 import pytest
 
-from test_gpu_orthogonalize import falling, lay_out, noise, rel, steps_of
+from test_gpu_orthogonalize import SHAPES, falling, lay_out, noise, rel, steps_of
 
 pytestmark = pytest.mark.gpu
 
@@ -61,3 +61,30 @@ def test_pairs_keep_their_bits(what):
         for out, want in results(FORMS[what], torch.float32, make):
             if out.numel() >= 256:
                 assert rel(out, want) <= 2.0 ** -19, tuple(out.shape)
+
+
+@pytest.mark.parametrize("what", sorted(SHAPES))
+def test_high_parts_around_every_forms_limits(what):
+    import torch
+    from paper_2204_08211_amd import binding as B
+    for make in (noise, falling):
+        for out, want in results(SHAPES[what], torch.float16, make, products=B.PRODUCTS_HIGH):
+            off = 2.0 ** -8 if out.numel() >= 256 else 2.0 ** -5
+            assert rel(out, want) <= rel(want.half(), want) + 2 * off, tuple(out.shape)
+
+
+@pytest.mark.parametrize("bad", [(60, 30), (40, 300), (70, 200)])
+def test_high_parts_of_zeros_and_values_that_are_not_finite(bad):
+    import torch
+    from paper_2204_08211_amd import binding as B
+    size = bad[0] * bad[1]
+    g = torch.randn(4 * size, device="cuda:0").bfloat16()
+    g[:size] = 0
+    g[size + 5] = float("nan")
+    g[2 * size + 7] = float("inf")
+    status = torch.zeros(B.STATUS_WORDS, dtype=torch.int64, device="cuda:0")
+    plan = B.MatrixPlan([(k * size,) + bad for k in range(4)], dtype=torch.bfloat16, products=B.PRODUCTS_HIGH)
+    out = B.co3_orthogonalize(plan, g, status=status)
+    assert bool((out[:size] == 0).all()) and bool(torch.isnan(out[size:3 * size]).all()) and int(status[B.STAT_NONFINITE]) == 2
+    want = steps_of(g[3 * size:].view(bad))
+    assert rel(out[3 * size:].view(bad), want) <= rel(want.bfloat16(), want) + 2 * 2.0 ** -8
