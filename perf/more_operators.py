@@ -117,18 +117,21 @@ def _from_8_bits(values, scale, block_rows):
 
 
 def _stored(x, block_rows=BLOCK):
-    """What a program keeps of x: the values' bytes, rows 16 bytes aligned and filled up with zeros, and the scales' bytes."""
+    """What a program keeps of x: the values' bytes, rows 16 bytes aligned and filled up with zeros, and the scales' bytes, those of a
+    column of blocks next to each other, 16 bytes aligned and filled up too."""
     values, scale = _to_8_bits(x.float(), block_rows)
     users, rows, cols = x.shape
     whole = torch.zeros((users, rows, _ceil(cols, 16) * 16), dtype=torch.uint8, device=x.device)
     whole[:, :, :cols] = values.contiguous().view(torch.uint8)
-    return dict(values=whole, scales=(scale + 127).to(torch.uint8), cols=cols, block_rows=block_rows)
+    scales = torch.nn.functional.pad((scale + 127).to(torch.uint8).mT, (0, -scale.shape[1] % 16)).contiguous()
+    return dict(values=whole, scales=scales, cols=cols, block_rows=block_rows)
 
 
 def _numbers(kept):
     """fp32 of what _stored gives."""
     values = kept["values"][:, :, :kept["cols"]].contiguous().view(torch.float8_e4m3fn)
-    return _from_8_bits(values, kept["scales"].int() - 127, kept["block_rows"])
+    scale = kept["scales"][:, :, :_ceil(values.shape[1], kept["block_rows"])].mT.int() - 127
+    return _from_8_bits(values, scale, kept["block_rows"])
 
 
 def _activations(gen, dev, users, rows, cols):
@@ -302,7 +305,7 @@ def _exact_numbers(values, scales, block_rows):
     size = torch.where(v >= 128, -size, size)
     row = torch.arange(v.shape[1], device=v.device) // block_rows
     col = torch.arange(v.shape[2], device=v.device) // BLOCK
-    return size * torch.pow(2.0, scales.double() - 127)[:, row][:, :, col]
+    return size * torch.pow(2.0, scales.mT.double() - 127)[:, row][:, :, col]
 
 
 def _exact_rounded(x):
