@@ -458,6 +458,125 @@ typedef struct {
 size_t co3_layernorm_backward_workspace_bytes(uint32_t U, uint64_t rows_per_user, uint32_t cols);
 int co3_layernorm_backward(const co3_layernorm_backward_args *args, void *stream);
 
+/* ---- activations and products in 8 bits ---------------------------------------------------
+ * Matrices of e4m3 numbers (a sign, 4 bits of an exponent, 3 of a fraction, no infinities) with a power of two as the scale of
+ * each block of 128 columns by block_rows rows, 128 or 1; x = value 2^(scale - 127).  Blocks of 128 rows can be read along
+ * either side: one copy of an activation serves the forward product, waits for the backward pass in a byte an element, and
+ * serves the weight's gradient there.  Every matrix of a batch has blocks of its own.
+ * The bytes of a row from cols up to the next multiple of 16 are zeros (co3_quantize8 writes them).                     */
+typedef struct {
+    uint8_t *values;         /* device, 16-byte aligned: row r of matrix i begins at byte i batch_stride + r ld         */
+    uint8_t *scales;         /* device, 16-byte aligned: [batch][ceil(cols / 128)][scale_ld], a block row's at its number */
+    uint64_t rows;           /* 0 .. 2^31 - 1                                                  */
+    uint64_t ld;             /* a multiple of 16, >= cols, <= CO3_MAX_BLOCKS8_LD               */
+    uint64_t batch_stride;   /* a multiple of 16, where batch > 1 >= the bytes of a matrix     */
+    uint32_t cols;           /* 1 .. CO3_MAX_BLOCKS8_COLS                                      */
+    uint32_t batch;          /* 1 .. 65535                                                     */
+    uint32_t block_rows;     /* 128 or 1                                                       */
+    uint32_t scale_ld;       /* a multiple of 16, >= ceil(rows / block_rows)                   */
+} co3_blocks8;
+#define CO3_MAX_BLOCKS8_COLS (1u << 20)
+#define CO3_MAX_BLOCKS8_LD (1u << 22)
+
+/* To 8 bits.  A block's scale is the least power of two, of 2^-126 at least, by which its largest finite value is at most 448 (1 for a
+ * block of zeros); the values are rounded to the nearest, ties to even.  NaN and infinities become NaN, and are counted in
+ * status[CO3_STAT_NONFINITE] where status is given.                                                                     */
+typedef struct {
+    const void *x;           /* device: row r of matrix i begins at element i x_batch_stride + r x_stride                */
+    co3_blocks8 out;         /* neither may lie where x does                                   */
+    uint64_t x_stride;       /* >= cols                                                        */
+    uint64_t x_batch_stride;
+    uint64_t *status;        /* device [CO3_STATUS_WORDS] counters (added to), or NULL         */
+    int32_t type;            /* of x                                                           */
+    int32_t reserved;
+} co3_quantize8_args;
+int co3_quantize8(const co3_quantize8_args *args, void *stream);
+
+/* And back: the values that are stored, those beyond the type's range at its ends.  Elements between the rows stay.     */
+typedef struct {
+    co3_blocks8 x;
+    void *out;
+    uint64_t out_stride;     /* >= cols                                                        */
+    uint64_t out_batch_stride;
+    int32_t type;            /* of out                                                         */
+    int32_t reserved;
+} co3_dequantize8_args;
+int co3_dequantize8(const co3_dequantize8_args *args, void *stream);
+
+/* out = op(a) op(b), or out + op(a) op(b) with accumulate, for every matrix of a batch: [m][k] by [k][n], op the transpose where
+ * asked for.  a and b have the same batch, or one of them a single matrix for all of the other's.  y = x W^T of a layer's weights
+ * W [outputs][inputs], dx = dy W and, for every user, dW = dy^T x: `out` may be a layer's part of the users' gradients that
+ * co3_encode reads.  Where the sum runs along the rows (a transposed, b not) the blocks have 128 rows.
+ * Sums are fp32 and rounded once.  Results of 16 bits are made by the matrix instructions for 8-bit numbers, which add sixteen
+ * products at a time, cut off at some 2^-16 of the largest (2e-5 to 7e-5 of the result, a hundredth of its rounding to bf16); those
+ * of fp32 by the instructions for bf16, in which these numbers, and their products in fp32, are exact (numbers below 2^-126 may count
+ * as zeros there).  k = 0 gives zeros.
+ * workspace: device, co3_matmul8_workspace_bytes() of these args, 16-byte aligned; NULL where that is 0.                */
+typedef struct {
+    co3_blocks8 a, b;
+    void *out;               /* device: row r of matrix i begins at element i out_batch_stride + r out_stride            */
+    uint64_t out_stride;     /* >= n                                                           */
+    uint64_t out_batch_stride;
+    int32_t type;            /* of out                                                         */
+    int32_t transpose_a, transpose_b;
+    int32_t accumulate;
+    void *workspace;
+    size_t workspace_bytes;
+} co3_matmul8_args;
+size_t co3_matmul8_workspace_bytes(const co3_matmul8_args *args);   /* 0 for args that co3_matmul8 refuses; out and workspace are not looked at */
+int co3_matmul8(const co3_matmul8_args *args, void *stream);
+
+/* Group norm with an activation, channels last: pixel p of sample i is row i pixels + p.  Over the pixels and the channels
+ * of a group (channels / groups next to each other):  mean, var (biased), rstd = 1 / sqrt(var + eps),
+ * z = (x - mean) rstd weight + bias,  y = act(z): z, max(z, 0) or z / (1 + exp(-z)).
+ * weight and bias (fp32 [channels]) may each be NULL (1 and 0), mean and rstd (fp32 [samples][groups]) too.  y may be x.
+ * The stream's and the tensors' GPU is the current one, here and in the backward pass.
+ * workspace: device, co3_groupnorm_workspace_bytes(), 16-byte aligned; NULL where that is 0.                            */
+enum { CO3_ACT_NONE = 0, CO3_ACT_RELU = 1, CO3_ACT_SILU = 2 };
+typedef struct {
+    const void *x;
+    void *y;
+    const float *weight, *bias;
+    float *mean, *rstd;
+    uint64_t samples, pixels;        /* pixels >= 1; samples pixels <= 2^31 - 1                */
+    uint64_t x_stride, y_stride;     /* elements between pixels, >= channels                   */
+    uint32_t channels, groups;       /* 1 .. CO3_MAX_NORM_COLS; groups divides channels        */
+    int32_t type;
+    int32_t activation;
+    float eps;
+    int32_t reserved;
+    void *workspace;
+    size_t workspace_bytes;
+} co3_groupnorm_args;
+size_t co3_groupnorm_workspace_bytes(uint64_t samples, uint64_t pixels, uint32_t channels, uint32_t groups, int32_t type);
+int co3_groupnorm(const co3_groupnorm_args *args, void *stream);
+
+/* Its backward pass for U users of samples_per_user samples each:
+ *   xh = (x - mean) rstd,  z = xh weight + bias,  dz = dy act'(z),  t = dz weight,  dx = rstd (t - mean(t) - xh mean(t xh)), the means
+ *   over the group;  dweight[u] = sum over the user's pixels of dz xh,  dbias[u] = sum of dz, in a fixed order.
+ * x is given in `type`, or (x NULL) in 8 bits, x8: `batch` = U matrices of samples_per_user pixels rows, or one of all.
+ * dweight, dbias, grad_stride, accumulate as in co3_layernorm_backward.  dx may be dy or x.                             */
+typedef struct {
+    const void *dy, *x;
+    void *dx;
+    co3_blocks8 x8;
+    const float *weight, *bias;
+    const float *mean, *rstd;
+    float *dweight, *dbias;
+    uint64_t grad_stride;            /* >= channels where U > 1                                */
+    uint64_t samples_per_user, pixels;   /* pixels >= 1; U samples_per_user pixels <= 2^31 - 1 */
+    uint64_t dy_stride, x_stride, dx_stride;
+    uint32_t U;                      /* 1 .. 65535                                             */
+    uint32_t channels, groups;
+    int32_t type;
+    int32_t activation;
+    int32_t accumulate;
+    void *workspace;
+    size_t workspace_bytes;
+} co3_groupnorm_backward_args;
+size_t co3_groupnorm_backward_workspace_bytes(uint32_t U, uint64_t samples_per_user, uint64_t pixels, uint32_t channels, uint32_t groups, int32_t type);
+int co3_groupnorm_backward(const co3_groupnorm_backward_args *args, void *stream);
+
 /* ---- measurement aid ---------------------------------------------------------------------
  * Between co3_profile_begin() and co3_profile_end() every kernel the library launches is
  * bracketed by two HIP events recorded on the stream it is launched on.  co3_profile_end

@@ -33,6 +33,8 @@ EXPORTS = [
     "co3_plan_bias_workspace_bytes", "co3_set_lookback_polls", "co3_encode_static", "co3_plan_set_gain",
     "co3_matrix_plan_create", "co3_matrix_plan_destroy", "co3_matrix_plan_workspace_bytes", "co3_matrix_plan_elements",
     "co3_orthogonalize", "co3_muon_update", "co3_layernorm", "co3_layernorm_backward_workspace_bytes", "co3_layernorm_backward",
+    "co3_quantize8", "co3_dequantize8", "co3_matmul8_workspace_bytes", "co3_matmul8", "co3_groupnorm_workspace_bytes", "co3_groupnorm",
+    "co3_groupnorm_backward_workspace_bytes", "co3_groupnorm_backward",
 ]
 
 
@@ -99,19 +101,58 @@ class LayernormBackwardArgs(C.Structure):
                 ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
 
 
+class Blocks8Struct(C.Structure):
+    _fields_ = [("values", C.c_void_p), ("scales", C.c_void_p), ("rows", C.c_uint64), ("ld", C.c_uint64), ("batch_stride", C.c_uint64),
+                ("cols", C.c_uint32), ("batch", C.c_uint32), ("block_rows", C.c_uint32), ("scale_ld", C.c_uint32)]
+
+
+class Quantize8Args(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("out", Blocks8Struct), ("x_stride", C.c_uint64), ("x_batch_stride", C.c_uint64), ("status", C.c_void_p),
+                ("type", C.c_int32), ("reserved", C.c_int32)]
+
+
+class Dequantize8Args(C.Structure):
+    _fields_ = [("x", Blocks8Struct), ("out", C.c_void_p), ("out_stride", C.c_uint64), ("out_batch_stride", C.c_uint64), ("type", C.c_int32),
+                ("reserved", C.c_int32)]
+
+
+class Matmul8Args(C.Structure):
+    _fields_ = [("a", Blocks8Struct), ("b", Blocks8Struct), ("out", C.c_void_p), ("out_stride", C.c_uint64), ("out_batch_stride", C.c_uint64),
+                ("type", C.c_int32), ("transpose_a", C.c_int32), ("transpose_b", C.c_int32), ("accumulate", C.c_int32),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
+class GroupnormArgs(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("y", C.c_void_p), ("weight", C.c_void_p), ("bias", C.c_void_p), ("mean", C.c_void_p), ("rstd", C.c_void_p),
+                ("samples", C.c_uint64), ("pixels", C.c_uint64), ("x_stride", C.c_uint64), ("y_stride", C.c_uint64), ("channels", C.c_uint32),
+                ("groups", C.c_uint32), ("type", C.c_int32), ("activation", C.c_int32), ("eps", C.c_float), ("reserved", C.c_int32),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
+class GroupnormBackwardArgs(C.Structure):
+    _fields_ = [("dy", C.c_void_p), ("x", C.c_void_p), ("dx", C.c_void_p), ("x8", Blocks8Struct), ("weight", C.c_void_p), ("bias", C.c_void_p),
+                ("mean", C.c_void_p), ("rstd", C.c_void_p), ("dweight", C.c_void_p), ("dbias", C.c_void_p), ("grad_stride", C.c_uint64),
+                ("samples_per_user", C.c_uint64), ("pixels", C.c_uint64), ("dy_stride", C.c_uint64), ("x_stride", C.c_uint64),
+                ("dx_stride", C.c_uint64), ("U", C.c_uint32), ("channels", C.c_uint32), ("groups", C.c_uint32), ("type", C.c_int32),
+                ("activation", C.c_int32), ("accumulate", C.c_int32), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
 _CODES = {C.c_void_p: "P", C.c_uint64: "Q", C.c_uint32: "I", C.c_int32: "i", C.c_float: "f", C.c_size_t: "N"}
 
 
 def _packer(struct_type):
     """struct.Struct.pack of a structure's fields in their order (0 for a null pointer): the same bytes as the ctypes
     structure, in a third of the time; calls of a few microseconds are made with it."""
-    p = struct.Struct("@" + "".join(_CODES[t] for _, t in struct_type._fields_) + "0Q")
+    codes = "".join(_CODES.get(t) or "".join(_CODES[f] for _, f in t._fields_) for _, t in struct_type._fields_)
+    p = struct.Struct("@" + codes + "0Q")
     assert p.size == C.sizeof(struct_type)
     return p.pack
 
 
 _pack_orthogonalize, _pack_muon = _packer(OrthogonalizeArgs), _packer(MuonArgs)
 _pack_layernorm, _pack_layernorm_backward = _packer(LayernormArgs), _packer(LayernormBackwardArgs)
+_pack_quantize8, _pack_dequantize8, _pack_matmul8 = _packer(Quantize8Args), _packer(Dequantize8Args), _packer(Matmul8Args)
+_pack_groupnorm, _pack_groupnorm_backward = _packer(GroupnormArgs), _packer(GroupnormBackwardArgs)
 
 
 class KernelTime(C.Structure):
@@ -191,6 +232,13 @@ def lib():
         L.co3_layernorm_backward_workspace_bytes.argtypes = [C.c_uint32, C.c_uint64, C.c_uint32]
         L.co3_layernorm_backward_workspace_bytes.restype = C.c_size_t
         L.co3_layernorm_backward.argtypes = [C.c_void_p, C.c_void_p]
+        for name in ("co3_quantize8", "co3_dequantize8", "co3_matmul8", "co3_groupnorm", "co3_groupnorm_backward"):
+            getattr(L, name).argtypes = [C.c_void_p, C.c_void_p]
+        L.co3_matmul8_workspace_bytes.argtypes = [C.c_void_p]
+        L.co3_groupnorm_workspace_bytes.argtypes = [C.c_uint64, C.c_uint64, C.c_uint32, C.c_uint32, C.c_int32]
+        L.co3_groupnorm_backward_workspace_bytes.argtypes = [C.c_uint32, C.c_uint64, C.c_uint64, C.c_uint32, C.c_uint32, C.c_int32]
+        for name in ("co3_matmul8_workspace_bytes", "co3_groupnorm_workspace_bytes", "co3_groupnorm_backward_workspace_bytes"):
+            getattr(L, name).restype = C.c_size_t
         L.co3_status_string.argtypes = [C.c_int]
         L.co3_status_string.restype = C.c_char_p
         _lib = L
@@ -773,4 +821,251 @@ def co3_layernorm_backward(dy, x, weight, mean, rstd, dx=None, dweight=None, dbi
                               0 if workspace is None else workspace.nbytes)
     on = _stream_of(gpu, stream)
     _check("co3_layernorm_backward", _call_on(gpu, lib().co3_layernorm_backward, a, on))
+    return dx
+
+
+# ---- activations and products in 8 bits, group norm ----
+
+BLOCK_COLS = 128
+MAX_BLOCKS8_COLS, MAX_BLOCKS8_LD = 1 << 20, 1 << 22
+ACT_NONE, ACT_RELU, ACT_SILU = 0, 1, 2
+
+
+class Blocks8:
+    """co3_blocks8: a batch of matrices [rows, cols] of e4m3 numbers with a power of two for each block of 128 columns by block_rows (128 or
+    1) rows.  values: uint8 [batch, rows, ld], rows 16 bytes aligned, zeros from cols up to the next multiple of 16; scales: uint8
+    [batch, ceil(cols / 128), ceil(rows / block_rows) rounded up to a multiple of 16], 2^(byte - 127).  For a program that keeps
+    one: co3_quantize8 writes both."""
+
+    __slots__ = ("values", "scales", "batch", "rows", "cols", "block_rows", "gpu", "_fields")
+
+    def __init__(self, values, scales, cols, block_rows=128):
+        import torch
+        if values.dtype is not torch.uint8 or scales.dtype is not torch.uint8 or values.dim() != 3 or scales.dim() != 3:
+            raise ValueError("values [batch, rows, ld] and scales [batch, columns of blocks, ...] of uint8 are taken")
+        batch, rows, ld = values.shape
+        blocks, columns = (rows + block_rows - 1) // block_rows if block_rows in (1, 128) else -1, (int(cols) + BLOCK_COLS - 1) // BLOCK_COLS
+        if blocks < 0:
+            raise ValueError("block_rows: 128 or 1 is taken")
+        if not 1 <= cols <= min(ld, MAX_BLOCKS8_COLS) or not 1 <= batch <= 65535:
+            raise ValueError("values: 1 to 65535 matrices whose rows have room for the columns are taken")
+        stride = values.stride(1) if rows > 1 else ld
+        if (ld > 1 and values.stride(2) != 1) or stride % 16 or stride < ld or ld % 16 or stride > MAX_BLOCKS8_LD or values.data_ptr() % 16 or \
+                (batch > 1 and values.stride(0) % 16):
+            raise ValueError("values: rows of contiguous bytes at 16-byte addresses are taken")
+        if scales.shape[0] != batch or scales.shape[1] != columns or scales.shape[2] < blocks or scales.shape[2] % 16 or not scales.is_contiguous() or \
+                scales.data_ptr() % 16 or scales.get_device() != values.get_device():
+            raise ValueError(f"scales: contiguous [{batch}, {columns}, {(blocks + 15) // 16 * 16}] at a 16-byte address of the values' device are taken")
+        self.values, self.scales = values, scales
+        self.batch, self.rows, self.cols, self.block_rows, self.gpu = batch, rows, int(cols), block_rows, values.get_device()
+        self._fields = (values.data_ptr(), scales.data_ptr(), rows, stride, values.stride(0) if batch > 1 else rows * stride, self.cols, batch, block_rows,
+                        scales.shape[2])
+
+    @classmethod
+    def empty(cls, batch, rows, cols, block_rows=128, device="cuda"):
+        """One to be written."""
+        import torch
+        if block_rows not in (1, 128):
+            raise ValueError("block_rows: 128 or 1 is taken")
+        values = torch.empty((batch, rows, (cols + 15) // 16 * 16), dtype=torch.uint8, device=device)
+        blocks = (rows + block_rows - 1) // block_rows
+        scales = torch.empty((batch, (cols + BLOCK_COLS - 1) // BLOCK_COLS, (blocks + 15) // 16 * 16), dtype=torch.uint8, device=device)
+        return cls(values, scales, cols, block_rows)
+
+    @property
+    def shape(self):
+        return (self.batch, self.rows, self.cols)
+
+
+_NO_BLOCKS8 = (0,) * 9
+
+
+def _matrices(t, name):
+    """(batch, rows, columns, elements between rows, elements between matrices) of [rows, cols] or [batch, rows, cols]."""
+    shape, strides = t.shape, t.stride()
+    if len(shape) == 2:
+        (rows, cols), batch, between = shape, 1, 0
+    elif len(shape) == 3:
+        batch, rows, cols = shape
+        between = strides[0] if batch > 1 else 0
+    else:
+        raise ValueError(f"{name}: [rows, cols] or [batch, rows, cols] is taken")
+    if cols > 1 and strides[-1] != 1:
+        raise ValueError(f"{name}: rows have to be contiguous")
+    return batch, rows, cols, strides[-2] if rows > 1 else cols, between
+
+
+def co3_quantize8(x, out=None, block_rows=128, status=None, stream=None):
+    """Blocks8 of x [rows, cols] or [batch, rows, cols] (float32, bfloat16, float16; rows may lie apart), into `out` if given.  status (int64
+    [STATUS_WORDS], or None): values that are not finite, which become NaN, are added to status[STAT_NONFINITE]."""
+    batch, rows, cols, stride, between = _matrices(x, "x")
+    kind, gpu = tensor_type(x.dtype), x.get_device()
+    on = _stream_of(gpu, stream)
+    if out is None:
+        with _allocate_on(stream):
+            out = Blocks8.empty(batch, rows, cols, block_rows, x.device)
+    elif out.batch != batch or out.rows != rows or out.cols != cols or out.gpu != gpu:
+        raise ValueError("out: the shape and device of x are taken")
+    if status is not None and (status.get_device() != gpu or status.numel() < STATUS_WORDS or status.element_size() != 8 or not status.is_contiguous()):
+        raise ValueError(f"status: {STATUS_WORDS} contiguous int64 elements on x's GPU are taken")
+    a = _pack_quantize8(x.data_ptr(), *out._fields, stride, between, 0 if status is None else status.data_ptr(), kind, 0)
+    _check("co3_quantize8", _call_on(gpu, lib().co3_quantize8, a, on))
+    return out
+
+
+def co3_dequantize8(x, out=None, dtype=None, stream=None):
+    """The numbers of a Blocks8, [batch, rows, cols] of `dtype` (bfloat16 if not given) or into `out`."""
+    on = _stream_of(x.gpu, stream)
+    if out is None:
+        import torch
+        with _allocate_on(stream):
+            out = torch.empty(x.shape, dtype=torch.bfloat16 if dtype is None else dtype, device=x.values.device)
+    batch, rows, cols, stride, between = _matrices(out, "out")
+    if batch != x.batch or rows != x.rows or cols != x.cols or out.get_device() != x.gpu:
+        raise ValueError("out: the shape and device of x are taken")
+    a = _pack_dequantize8(*x._fields, out.data_ptr(), stride, between, tensor_type(out.dtype), 0)
+    _check("co3_dequantize8", _call_on(x.gpu, lib().co3_dequantize8, a, on))
+    return out
+
+
+def co3_matmul8_workspace_bytes(a, b, transpose_a=False, transpose_b=False):
+    return int(lib().co3_matmul8_workspace_bytes(_pack_matmul8(*a._fields, *b._fields, 0, 0, 0, F32, bool(transpose_a), bool(transpose_b), 0, 0, 0)))
+
+
+def co3_matmul8(a, b, out=None, dtype=None, transpose_a=False, transpose_b=False, accumulate=False, workspace=None, stream=None):
+    """op(a) op(b) of two Blocks8, for every matrix of a batch (one of them may be a single matrix for all of the other's), [batch, m, n] of
+    `dtype` (bfloat16 if not given) or into `out`, which may be a layer's part of the users' gradients; added to `out` with
+    accumulate.  Where the sum runs along the rows (a transposed, b not) blocks have 128 rows.  Results of 16 bits are made by the
+    8-bit matrix instructions; float32 ones are exact products, added in fp32."""
+    m, k = (a.cols, a.rows) if transpose_a else (a.rows, a.cols)
+    k2, n = (b.cols, b.rows) if transpose_b else (b.rows, b.cols)
+    if k != k2:
+        raise ValueError(f"a and b: sums of {k} and of {k2} terms do not fit")
+    if a.gpu != b.gpu:
+        raise ValueError("a and b: one device is taken")
+    if out is None and accumulate:
+        raise ValueError("out: there is nothing to add to")
+    batch = a.batch if a.batch > b.batch else b.batch
+    on = _stream_of(a.gpu, stream)
+    if out is None or workspace is None:
+        import torch
+        with _allocate_on(stream):
+            if out is None:
+                out = torch.empty((batch, m, n), dtype=torch.bfloat16 if dtype is None else dtype, device=a.values.device)
+            if workspace is None:
+                workspace = torch.empty(co3_matmul8_workspace_bytes(a, b, transpose_a, transpose_b), dtype=torch.uint8, device=a.values.device)
+    out_batch, rows, cols, stride, between = _matrices(out, "out")
+    if out_batch != batch or rows != m or cols != n or out.get_device() != a.gpu:
+        raise ValueError(f"out: [{batch}, {m}, {n}] on the device of a is taken")
+    if workspace.get_device() != a.gpu or not workspace.is_contiguous():
+        raise ValueError("workspace: contiguous memory of a's GPU is taken")
+    p = _pack_matmul8(*a._fields, *b._fields, out.data_ptr(), stride, between, tensor_type(out.dtype), 1 if transpose_a else 0, 1 if transpose_b else 0,
+                      1 if accumulate else 0, workspace.data_ptr(), workspace.nbytes)
+    _check("co3_matmul8", _call_on(a.gpu, lib().co3_matmul8, p, on))
+    return out
+
+
+def _images(t, name):
+    """(samples, pixels, channels, elements between pixels) of [samples, pixels, channels]."""
+    if t.dim() != 3:
+        raise ValueError(f"{name}: [samples, pixels, channels] is taken")
+    samples, pixels, channels = t.shape
+    if t.is_contiguous():
+        return samples, pixels, channels, channels
+    if channels > 1 and t.stride(2) != 1:
+        raise ValueError(f"{name}: channels have to lie next to each other")
+    stride = t.stride(1) if pixels > 1 else t.stride(0) if samples > 1 else channels
+    if samples > 1 and pixels > 1 and t.stride(0) != pixels * stride:
+        raise ValueError(f"{name}: all pixels have to lie the same distance apart")
+    return samples, pixels, channels, stride
+
+
+def _images_like(t, shape, dtype, name, gpu):
+    """Elements between the pixels of a tensor of that shape and type."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != gpu:
+        raise ValueError(f"{name}: {list(shape)} of {dtype} on the same device is taken")
+    return shape[-1] if t.is_contiguous() else _images(t, name)[3]
+
+
+def co3_groupnorm_workspace_bytes(samples, pixels, channels, groups, dtype):
+    return int(lib().co3_groupnorm_workspace_bytes(int(samples), int(pixels), int(channels), int(groups), tensor_type(dtype)))
+
+
+def co3_groupnorm_backward_workspace_bytes(users, samples, pixels, channels, groups, dtype):
+    """samples: those of all users."""
+    return int(lib().co3_groupnorm_backward_workspace_bytes(int(users), int(samples) // int(users), int(pixels), int(channels), int(groups), tensor_type(dtype)))
+
+
+def co3_groupnorm(x, groups, weight=None, bias=None, eps=1e-5, activation=ACT_NONE, y=None, mean=None, rstd=None, workspace=None, stream=None):
+    """(y, mean, rstd) of x [samples, pixels, channels] (float32, bfloat16, float16; an image's height and width are its pixels; pixels may
+    lie apart): y = act(norm weight + bias) of x's type, mean and rstd float32 [samples, groups].  weight, bias: float32 [channels] or
+    None.  activation: ACT_NONE, ACT_RELU or ACT_SILU.  y may be x."""
+    samples, pixels, channels, stride = _images(x, "x")
+    shape, dtype, gpu, f32 = x.shape, x.dtype, x.get_device(), _float32()
+    kind = tensor_type(dtype)
+    if groups < 1 or channels % groups:
+        raise ValueError(f"groups: a divisor of {channels} is taken")
+    if y is None or mean is None or rstd is None or workspace is None:
+        import torch
+        with _allocate_on(stream):
+            y = torch.empty(shape, dtype=dtype, device=x.device) if y is None else y
+            mean = torch.empty((samples, groups), dtype=f32, device=x.device) if mean is None else mean
+            rstd = torch.empty((samples, groups), dtype=f32, device=x.device) if rstd is None else rstd
+            if workspace is None:
+                workspace = torch.empty(co3_groupnorm_workspace_bytes(samples, pixels, channels, groups, dtype), dtype=torch.uint8, device=x.device)
+    if workspace.get_device() != gpu or not workspace.is_contiguous():
+        raise ValueError("workspace: contiguous memory of x's GPU is taken")
+    a = _pack_groupnorm(x.data_ptr(), y.data_ptr(), _norm_vector(weight, channels, "weight", gpu, f32), _norm_vector(bias, channels, "bias", gpu, f32),
+                        _norm_vector(mean, samples * groups, "mean", gpu, f32), _norm_vector(rstd, samples * groups, "rstd", gpu, f32), samples, pixels,
+                        stride, _images_like(y, shape, dtype, "y", gpu), channels, groups, kind, activation, float(eps), 0, workspace.data_ptr(),
+                        workspace.nbytes)
+    on = _stream_of(gpu, stream)
+    _check("co3_groupnorm", _call_on(gpu, lib().co3_groupnorm, a, on))
+    return y, mean, rstd
+
+
+def co3_groupnorm_backward(dy, x, groups, weight, bias, mean, rstd, activation=ACT_NONE, users=1, dx=None, dweight=None, dbias=None, accumulate=False,
+                           workspace=None, stream=None):
+    """dx of co3_groupnorm, and where dweight / dbias are given (float32 [users, channels], rows may lie apart: a layer's part of the
+    users' gradients that co3_encode reads) the weight's gradients of every user, who has samples / users of them: written, or added
+    with accumulate.  x: a tensor like dy, or the Blocks8 [users, samples / users * pixels, channels] (or [1, all pixels, channels])
+    that was kept of it."""
+    samples, pixels, channels, dy_stride = _images(dy, "dy")
+    shape, dtype, gpu, f32 = dy.shape, dy.dtype, dy.get_device(), _float32()
+    kind = tensor_type(dtype)
+    if users < 1 or samples % users:
+        raise ValueError(f"users: a divisor of {samples} samples is taken")
+    if groups < 1 or channels % groups:
+        raise ValueError(f"groups: a divisor of {channels} is taken")
+    stride = channels
+    if dweight is not None:
+        stride = _grad_rows(dweight, users, channels, "dweight", gpu, f32)
+    if dbias is not None:
+        other = _grad_rows(dbias, users, channels, "dbias", gpu, f32)
+        if dweight is not None and other != stride:
+            raise ValueError("dweight and dbias: the same distance between users is taken")
+        stride = other
+    if isinstance(x, Blocks8):
+        if x.gpu != gpu or x.cols != channels or x.batch not in (1, users) or x.batch * x.rows != samples * pixels:
+            raise ValueError(f"x: [{users}, {samples // users * pixels}, {channels}] in 8 bits on dy's device is taken")
+        at, x_stride, kept = 0, channels, x._fields
+    else:
+        at, x_stride, kept = x.data_ptr(), _images_like(x, shape, dtype, "x", gpu), _NO_BLOCKS8
+    if dx is None or workspace is None:
+        import torch
+        with _allocate_on(stream):
+            dx = torch.empty(shape, dtype=dtype, device=dy.device) if dx is None else dx
+            if workspace is None:
+                workspace = torch.empty(co3_groupnorm_backward_workspace_bytes(users, samples, pixels, channels, groups, dtype), dtype=torch.uint8,
+                                        device=dy.device)
+    if workspace.get_device() != gpu or not workspace.is_contiguous():
+        raise ValueError("workspace: contiguous memory of dy's GPU is taken")
+    a = _pack_groupnorm_backward(dy.data_ptr(), at, dx.data_ptr(), *kept, _norm_vector(weight, channels, "weight", gpu, f32),
+                                 _norm_vector(bias, channels, "bias", gpu, f32), _norm_vector(mean, samples * groups, "mean", gpu, f32),
+                                 _norm_vector(rstd, samples * groups, "rstd", gpu, f32), 0 if dweight is None else dweight.data_ptr(),
+                                 0 if dbias is None else dbias.data_ptr(), stride, samples // users, pixels, dy_stride, x_stride,
+                                 _images_like(dx, shape, dtype, "dx", gpu), users, channels, groups, kind, activation, 1 if accumulate else 0,
+                                 workspace.data_ptr(), workspace.nbytes)
+    on = _stream_of(gpu, stream)
+    _check("co3_groupnorm_backward", _call_on(gpu, lib().co3_groupnorm_backward, a, on))
     return dx

@@ -171,7 +171,8 @@ namespace co3 {
 // Per-kernel event timing (profile.cpp).  A ProfScope around a launch records two events on
 // the stream when profiling is on, and does nothing otherwise.
 enum KernelId { K_ZERO = 0, K_QUANTIZE, K_REDUCE_HIST, K_BUILD_BOOKS, K_CHUNK_BITS, K_SCAN, K_PACK, K_DECODE, K_AGGREGATE, K_FUSED, K_MOMENTS, K_FIT, K_MODEL_WEIGHTS, K_MODEL_BIAS,
-                K_ORTHO_NORM, K_ORTHO_PACK, K_ORTHO_GRAM, K_ORTHO_SQUARE, K_ORTHO_PRODUCT, K_ORTHO_SMALL, K_ORTHO_THIN, K_LAYERNORM, K_LAYERNORM_BACKWARD, K_LAYERNORM_GRAD, K_COUNT };
+                K_ORTHO_NORM, K_ORTHO_PACK, K_ORTHO_GRAM, K_ORTHO_SQUARE, K_ORTHO_PRODUCT, K_ORTHO_SMALL, K_ORTHO_THIN, K_LAYERNORM, K_LAYERNORM_BACKWARD, K_LAYERNORM_GRAD,
+                K_QUANTIZE8, K_DEQUANTIZE8, K_MATMUL8, K_MATMUL8_JOIN, K_GROUPNORM, K_GROUPNORM_SUMS, K_GROUPNORM_BACKWARD, K_GROUPNORM_GRAD, K_COUNT };
 bool profile_enabled();
 class ProfScope {
 public:
@@ -243,5 +244,16 @@ hipError_t launch_aggregate_wide(const Layout &lay, const co3_aggregate_args &a,
 hipError_t launch_layernorm(const co3_layernorm_args &a, hipStream_t s);
 size_t layernorm_backward_workspace_bytes(uint32_t U, uint64_t rows_per_user, uint32_t cols);
 hipError_t launch_layernorm_backward(const co3_layernorm_backward_args &a, hipStream_t s);
+// tensors in 8 bits (co3_train8.cpp, k_blocks8.hip, k_matmul8.hip)
+struct Matmul8Plan;
+bool valid_blocks8(const co3_blocks8 &b);
+hipError_t launch_quantize8(const co3_quantize8_args &a, hipStream_t s);
+hipError_t launch_dequantize8(const co3_dequantize8_args &a, hipStream_t s);
+hipError_t launch_matmul8(const co3_matmul8_args &a, const Matmul8Plan &plan, hipStream_t s);
+// group norm (k_groupnorm.hip)
+size_t groupnorm_workspace_bytes(uint64_t samples, uint64_t pixels, uint32_t channels, uint32_t groups, int32_t type);
+size_t groupnorm_backward_workspace_bytes(uint32_t U, uint64_t samples_per_user, uint64_t pixels, uint32_t channels, uint32_t groups, int32_t type);
+hipError_t launch_groupnorm(const co3_groupnorm_args &a, hipStream_t s);
+hipError_t launch_groupnorm_backward(const co3_groupnorm_backward_args &a, hipStream_t s);
 
 }  // namespace co3

@@ -1,0 +1,123 @@
+// Host side of the operators in 8 bits declared in include/co3.h: argument checks, how a product is cut into workgroups.
+#include <algorithm>
+#include <cmath>
+
+#include "blocks8.h"
+#include "co3_internal.h"
+#include "matmul8.h"
+#include "tensor_types.h"
+
+using namespace co3;
+
+namespace {
+
+constexpr uint64_t kMostStride = 1ull << 32, kMostBatchStride = 1ull << 46;   // so that the last element's index fits 64 bits
+
+inline bool aligned(const void *p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+inline bool valid_type(int32_t t) { return t == CO3_F32 || t == CO3_BF16 || t == CO3_F16; }
+
+// Whether rows of `cols` elements, `stride` apart, of a batch of matrices `batch_stride` apart, lie each by itself: one matrix behind
+// the other, or side by side in the same rows.
+bool apart(uint64_t rows, uint64_t cols, uint64_t stride, uint64_t batch, uint64_t batch_stride)
+{
+    if (rows == 0 || batch == 1) return true;
+    const uint64_t within = (rows - 1) * stride + cols, across = (batch - 1) * batch_stride + cols;
+    return batch_stride >= within || (batch_stride >= cols && stride >= across);
+}
+
+}  // namespace
+
+namespace co3 {
+
+bool valid_blocks8(const co3_blocks8 &b)
+{
+    if (b.cols == 0 || b.cols > CO3_MAX_BLOCKS8_COLS || b.rows >= (1ull << 31) || b.batch == 0 || b.batch > 65535u) return false;
+    if (b.ld < b.cols || b.ld % 16 || b.ld > CO3_MAX_BLOCKS8_LD || b.batch_stride % 16 || b.batch_stride > kMostBatchStride) return false;
+    if ((b.block_rows != 1 && b.block_rows != 128) || b.scale_ld % 16 || b.scale_ld < block_rows_of(b)) return false;
+    if (!aligned(b.values, 16) || !aligned(b.scales, 16)) return false;
+    if (b.rows == 0) return true;
+    const uint64_t wide = (b.cols + 15ull) & ~15ull;
+    return b.values && b.scales && apart(b.rows, wide, b.ld, b.batch, b.batch_stride);
+}
+
+}  // namespace co3
+
+namespace {
+
+// Checks a product and cuts it: CO3_OK and a plan, or what is wrong.
+int plan_matmul8(const co3_matmul8_args &a, Matmul8Plan *p)
+{
+    if (!valid_type(a.type) || !valid_blocks8(a.a) || !valid_blocks8(a.b)) return CO3_ERR_ARG;
+    const bool down_a = a.transpose_a != 0, down_b = a.transpose_b == 0;
+    const uint64_t m = down_a ? a.a.cols : a.a.rows, n = down_b ? a.b.cols : a.b.rows;
+    const uint64_t k = down_a ? a.a.rows : a.a.cols;
+    if (k != (down_b ? a.b.rows : a.b.cols)) return CO3_ERR_ARG;
+    if ((down_a && a.a.block_rows != 128) || (down_b && a.b.block_rows != 128)) return CO3_ERR_ARG;
+    if (a.a.batch != a.b.batch && a.a.batch != 1 && a.b.batch != 1) return CO3_ERR_ARG;
+    *p = {};
+    p->m = (uint32_t)m;
+    p->n = (uint32_t)n;
+    p->batch = std::max(a.a.batch, a.b.batch);
+    p->turns = (uint32_t)((k + 127) / 128);
+    if (m == 0 || n == 0) return CO3_OK;
+    const auto tiles = [&](uint64_t t) { return ((m + t - 1) / t) * ((n + t - 1) / t); };
+    p->form = tiles(256) * p->batch >= 256 ? 256 : 128;
+    p->tiles_m = (uint32_t)((m + p->form - 1) / p->form);
+    p->tiles_n = (uint32_t)((n + p->form - 1) / p->form);
+    const uint64_t all = tiles(p->form);
+    if (all > (1ull << 22)) return CO3_ERR_CAPACITY;   // fewer than 2^32 threads of a launch
+    p->tiles = (uint32_t)all;
+    p->part_ld = (uint32_t)((n + 3) & ~3ull);
+    const uint64_t groups = all * p->batch;
+    p->slices = p->turns == 0 ? 0u : (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(p->turns / 4, 512 / groups));
+    return CO3_OK;
+}
+
+size_t workspace_of(const Matmul8Plan &p)
+{
+    return p.slices > 1 ? (size_t)p.slices * p.batch * p.m * p.part_ld * sizeof(float) : 0;
+}
+
+}  // namespace
+
+extern "C" {
+
+int co3_quantize8(const co3_quantize8_args *a, void *stream)
+{
+    if (!a || !valid_type(a->type) || !valid_blocks8(a->out) || !aligned(a->status, 8)) return CO3_ERR_ARG;
+    if (a->out.rows == 0) return CO3_OK;
+    if (!a->x || !aligned(a->x, type_bytes(a->type)) || a->x_stride < a->out.cols || a->x_stride > kMostStride || a->x_batch_stride > kMostBatchStride) return CO3_ERR_ARG;
+    return launch_quantize8(*a, static_cast<hipStream_t>(stream)) == hipSuccess ? CO3_OK : CO3_ERR_HIP;
+}
+
+int co3_dequantize8(const co3_dequantize8_args *a, void *stream)
+{
+    if (!a || !valid_type(a->type) || !valid_blocks8(a->x)) return CO3_ERR_ARG;
+    if (a->x.rows == 0) return CO3_OK;
+    if (!a->out || !aligned(a->out, type_bytes(a->type)) || a->out_stride < a->x.cols || a->out_stride > kMostStride || a->out_batch_stride > kMostBatchStride) return CO3_ERR_ARG;
+    if (!apart(a->x.rows, a->x.cols, a->out_stride, a->x.batch, a->out_batch_stride)) return CO3_ERR_ARG;
+    return launch_dequantize8(*a, static_cast<hipStream_t>(stream)) == hipSuccess ? CO3_OK : CO3_ERR_HIP;
+}
+
+size_t co3_matmul8_workspace_bytes(const co3_matmul8_args *a)
+{
+    Matmul8Plan p;
+    return a && plan_matmul8(*a, &p) == CO3_OK ? workspace_of(p) : 0;
+}
+
+int co3_matmul8(const co3_matmul8_args *a, void *stream)
+{
+    if (!a) return CO3_ERR_ARG;
+    Matmul8Plan p;
+    if (const int rc = plan_matmul8(*a, &p); rc != CO3_OK) return rc;
+    if (p.m == 0 || p.n == 0) return CO3_OK;
+    if (!a->out || !aligned(a->out, type_bytes(a->type)) || a->out_stride < p.n || a->out_stride > kMostStride || a->out_batch_stride > kMostBatchStride) return CO3_ERR_ARG;
+    if (!apart(p.m, p.n, a->out_stride, p.batch, a->out_batch_stride)) return CO3_ERR_ARG;
+    if (const size_t need = workspace_of(p); need) {
+        if (!a->workspace || !aligned(a->workspace, 16)) return CO3_ERR_ARG;
+        if (a->workspace_bytes < need) return CO3_ERR_CAPACITY;
+    }
+    return launch_matmul8(*a, p, static_cast<hipStream_t>(stream)) == hipSuccess ? CO3_OK : CO3_ERR_HIP;
+}
+
+}  // extern "C"

@@ -23,6 +23,7 @@
 #include <type_traits>
 
 #include "co3_internal.h"
+#include "lds_loads.h"
 #include "ortho_device.h"
 
 namespace co3 {
@@ -157,21 +158,6 @@ template <int F> constexpr int kStage = 2 * Form<F>::T * kTurn;   // fp16 number
 // sixteen lanes read at a time, lie in different ones of the 64 banks.
 __device__ inline int exchanged(int row, int chunk) { return chunk ^ (row >> 2 & 3); }
 
-// 64 lanes' 16 bytes from memory to LDS, without a register in between: from base + offset (of every lane) + k, to `lds` + 16 lane.
-// Written out, since the compiler would wait for all loads to LDS before every read of LDS.  Who reads waits with wait_loads().
-// m0 is named for the compiler's own writes to it; no value lives there, which is what its warning is about.
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"
-__device__ inline void load_to_lds(u32x4 base, uint32_t offset, uint32_t k, uint32_t lds)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" : : "s"(lds), "v"(offset), "s"(base), "s"(k) : "m0", "memory");
-}
-#pragma clang diagnostic pop
-// Until all but the wavefront's last `left` loads are there.
-template <int left>
-__device__ inline void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" : : "n"(left) : "memory"); }
-
 // 32 columns from `col` on by 16 rows of a turn's blocks in LDS, as an operand whose rows the columns are: a lane gets eight rows of a
 // column.  Sixteen lanes read four rows of sixteen columns, four next to each other each, and are given four rows of one column.
 template <bool PAIR>
@@ -185,25 +171,6 @@ __device__ inline half8 read_down(const _Float16 *blocks, int across, int h, int
     typedef __attribute__((address_space(3))) short4v *lds4;
     const short4v low = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)at), high = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(at + 4 * 32));
     return __builtin_bit_cast(half8, (short8v)__builtin_shufflevector(low, high, 0, 1, 2, 3, 4, 5, 6, 7));
-}
-
-// All wavefronts of the workgroup, each with what it asked of LDS.  (__syncthreads() would wait for the loads to LDS as well.)
-__device__ inline void meet()
-{
-    asm volatile("" : : : "memory");
-    __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0)
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" : : : "memory");
-}
-
-// A buffer of `bytes` from p on, for load_to_lds.
-__device__ inline u32x4 buffer_of(const void *p, uint32_t bytes)
-{
-    const uint64_t at = reinterpret_cast<uint64_t>(p);
-    u32x4 r = {(uint32_t)at, (uint32_t)(at >> 32) & 0xffffu, bytes, 0x00027000u};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) r[i] = (uint32_t)__builtin_amdgcn_readfirstlane((int)r[i]);
-    return r;
 }
 
 // acc[i][j] += sum over k of P[i][k] Q[j][k] for a wavefront's part of the tile, from rows of K values, over `all` turns from `begin`
