@@ -12,7 +12,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libco3.so")
 SOURCES = ["co3_api.cpp", "host_codebook.cpp", "host_gennorm.cpp", "profile.cpp", "k_quantize.hip", "k_codebook.hip", "k_pack.hip", "k_fused.hip", "k_fit.hip", "k_decode.hip", "k_wide.hip", "k_decode_wide.hip",
            "co3_train.cpp", "k_ortho.hip", "k_ortho_small.hip", "k_layernorm.hip",
-           "co3_train8.cpp", "k_blocks8.hip", "k_matmul8.hip", "k_groupnorm.hip"]
+           "co3_train8.cpp", "k_blocks8.hip", "k_matmul8.hip", "k_groupnorm.hip", "k_groupnorm_backward.hip", "k_groupnorm_backward8.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
