@@ -473,7 +473,7 @@ typedef struct {
     uint32_t cols;           /* 1 .. CO3_MAX_BLOCKS8_COLS                                      */
     uint32_t batch;          /* 1 .. 65535                                                     */
     uint32_t block_rows;     /* 128 or 1                                                       */
-    uint32_t scale_ld;       /* a multiple of 16, >= ceil(rows / block_rows)                   */
+    uint32_t scale_ld;       /* a multiple of 16, >= ceil(rows / block_rows); ceil(cols / 128) scale_ld < 2^31 */
 } co3_blocks8;
 #define CO3_MAX_BLOCKS8_COLS (1u << 20)
 #define CO3_MAX_BLOCKS8_LD (1u << 22)

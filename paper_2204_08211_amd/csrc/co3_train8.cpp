@@ -34,7 +34,7 @@ bool valid_blocks8(const co3_blocks8 &b)
     if (b.cols == 0 || b.cols > CO3_MAX_BLOCKS8_COLS || b.rows >= (1ull << 31) || b.batch == 0 || b.batch > 65535u) return false;
     if (b.ld < b.cols || b.ld % 16 || b.ld > CO3_MAX_BLOCKS8_LD || b.batch_stride % 16 || b.batch_stride > kMostBatchStride) return false;
     if ((b.block_rows != 1 && b.block_rows != 128) || b.scale_ld % 16 || b.scale_ld < block_rows_of(b)) return false;
-    if (!aligned(b.values, 16) || !aligned(b.scales, 16)) return false;
+    if ((uint64_t)block_columns(b) * b.scale_ld >= (1ull << 31) || !aligned(b.values, 16) || !aligned(b.scales, 16)) return false;
     if (b.rows == 0) return true;
     const uint64_t wide = (b.cols + 15ull) & ~15ull;
     return b.values && b.scales && apart(b.rows, wide, b.ld, b.batch, b.batch_stride);
@@ -43,6 +43,26 @@ bool valid_blocks8(const co3_blocks8 &b)
 }  // namespace co3
 
 namespace {
+
+constexpr uint64_t kMostTiles = 1ull << 22;   // and slices, of a matrix: fewer than 2^32 threads of a launch
+
+// What a product of tiles takes, in microseconds: a turn of a workgroup by itself, and of all that the chip has room for at a time,
+// which share the caches; what comes before its turns and behind them; each for results of 16 bits and of fp32.
+// Measured (us; two rounds of workgroups and more by `full`, few of them by `alone`): 8192 x 4096 x 4096 bf16 256 118, 128 158; 4 times 4096^3 fp32 448, 494;
+// 8 times 500 x 1024 x 1000 bf16 256 20.5, 128 13.9, 64 18.8; 1000 x 517 x 1001 fp32 128 13.9, 64 8.0; 256 x 256 x 4096 bf16 64 12.2, in four slices 9.1.
+struct Rate8 { uint32_t form, room; double alone[2], full[2], ends[2]; };
+constexpr Rate8 kRates8[] = {{256, 256, {1.30, 1.60}, {1.80, 3.30}, {6.0, 12.0}},
+                             {128, 512, {0.65, 0.75}, {1.20, 1.90}, {4.0, 6.0}},
+                             {64, 512, {0.28, 0.35}, {0.80, 0.90}, {3.0, 3.5}}};
+
+double time_of(const Rate8 &rate, const Matmul8Plan &p, bool exact)
+{
+    const double groups = (double)p.tiles * p.slices * p.batch, rounds = std::ceil(groups / rate.room), busy = std::min(1.0, groups / rate.room);
+    const double turn = std::max(rate.alone[exact], rate.full[exact] * busy), turns = std::ceil((double)p.turns / p.slices);
+    // slices are written and read once more, by a launch of its own
+    const double join = p.slices > 1 ? 4.0 + 8.0 * p.slices * p.batch * p.m * (double)p.part_ld / 6e6 : 0.0;
+    return rounds * (rate.ends[exact] + turns * turn) + join;
+}
 
 // Checks a product and cuts it: CO3_OK and a plan, or what is wrong.
 int plan_matmul8(const co3_matmul8_args &a, Matmul8Plan *p)
@@ -60,16 +80,34 @@ int plan_matmul8(const co3_matmul8_args &a, Matmul8Plan *p)
     p->batch = std::max(a.a.batch, a.b.batch);
     p->turns = (uint32_t)((k + 127) / 128);
     if (m == 0 || n == 0) return CO3_OK;
-    const auto tiles = [&](uint64_t t) { return ((m + t - 1) / t) * ((n + t - 1) / t); };
-    p->form = tiles(256) * p->batch >= 256 ? 256 : 128;
-    p->tiles_m = (uint32_t)((m + p->form - 1) / p->form);
-    p->tiles_n = (uint32_t)((n + p->form - 1) / p->form);
-    const uint64_t all = tiles(p->form);
-    if (all > (1ull << 22)) return CO3_ERR_CAPACITY;   // fewer than 2^32 threads of a launch
-    p->tiles = (uint32_t)all;
     p->part_ld = (uint32_t)((n + 3) & ~3ull);
-    const uint64_t groups = all * p->batch;
-    p->slices = p->turns == 0 ? 0u : (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(p->turns / 4, 512 / groups));
+    const auto take = [&](uint32_t form, uint32_t high, uint32_t slices) {
+        const uint64_t all = ((m + high - 1) / high) * ((n + form - 1) / form);
+        if (all > kMostTiles || all * slices > kMostTiles) return false;
+        p->form = form;
+        p->tiles_m = (uint32_t)((m + high - 1) / high);
+        p->tiles_n = (uint32_t)((n + form - 1) / form);
+        p->tiles = (uint32_t)all;
+        p->slices = slices;
+        return true;
+    };
+    if (p->turns == 0) return take(256, 256, 0) ? CO3_OK : CO3_ERR_CAPACITY;
+    if (m <= 16 && !down_a && !down_b) return take(kFormRows, kFormRows, 1) ? CO3_OK : CO3_ERR_CAPACITY;
+    bool found = false;
+    double least = 0.0;
+    Matmul8Plan best = *p;
+    for (const Rate8 &rate : kRates8)
+        for (uint32_t slices = 1; slices <= p->turns && slices <= 32; slices += slices < 4 ? 1 : slices / 2) {
+            if (!take(rate.form, rate.form, slices)) continue;
+            const double time = time_of(rate, *p, a.type == CO3_F32);
+            if (!found || time < least) {
+                found = true;
+                least = time;
+                best = *p;
+            }
+        }
+    if (!found) return CO3_ERR_CAPACITY;
+    *p = best;
     return CO3_OK;
 }
 

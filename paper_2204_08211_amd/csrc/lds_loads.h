@@ -8,7 +8,7 @@ namespace co3 {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-// 64 lanes' 16 bytes: from base + offset (of every lane) + k, to `lds` + 16 lane; zeros where offset is not within the buffer.
+// 64 lanes' 16 bytes: from base + offset (of every lane) + k, to `lds` + 16 lane; zeros where offset + k is not within the buffer.
 // Written out, since the compiler would wait for all loads to LDS before every read of LDS.  Who reads waits with wait_loads().
 // m0 is named for the compiler's own writes to it; no value lives there, which is what its warning is about.
 #pragma clang diagnostic push
@@ -16,6 +16,11 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 __device__ inline void load_to_lds(u32x4 base, uint32_t offset, uint32_t k, uint32_t lds)
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" : : "s"(lds), "v"(offset), "s"(base), "s"(k) : "m0", "memory");
+}
+// 64 lanes' four bytes, to `lds` + 4 lane.
+__device__ inline void load_word_to_lds(u32x4 base, uint32_t offset, uint32_t k, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" : : "s"(lds), "v"(offset), "s"(base), "s"(k) : "m0", "memory");
 }
 #pragma clang diagnostic pop
 

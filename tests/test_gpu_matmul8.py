@@ -60,7 +60,7 @@ def compare(out, a, b, ta, tb, add=None):
 
 
 FORMS = [(False, True), (False, False), (True, False), (True, True)]
-SIZES = [(1, 1, 1), (1, 64, 128), (3, 5, 129), (31, 33, 127), (128, 128, 128), (129, 127, 16), (130, 257, 300), (16, 1000, 640), (255, 256, 1000), (300, 17, 2049)]
+SIZES = [(1, 1, 1), (1, 64, 128), (1, 40, 5000), (15, 65, 1040), (17, 33, 4000), (3, 5, 129), (31, 33, 127), (128, 128, 128), (129, 127, 16), (130, 257, 300), (16, 1000, 640), (255, 256, 1000), (300, 17, 2049)]
 
 
 @pytest.mark.parametrize("m,n,k", SIZES)
@@ -78,14 +78,14 @@ def test_forms(name, ta, tb, m, n, k):
         compare(out, a, b, ta, tb)
 
 
+@pytest.mark.parametrize("m,n,k", [(4001, 4100, 270), (4000, 4090, 1100), (700, 900, 5000)])
 @pytest.mark.parametrize("ta,tb", FORMS)
 @pytest.mark.parametrize("name", ["float32", "bfloat16"])
-def test_large_tiles(name, ta, tb):
-    """Enough tiles of 256 for all CUs, ragged at every end."""
+def test_large_tiles(name, ta, tb, m, n, k):
+    """Enough tiles of 128 and of 256 for all CUs, ragged at every end; long sums in slices."""
     from paper_2204_08211_amd import binding as B
     gen = torch.Generator(device="cuda:0")
     gen.manual_seed(7)
-    m, n, k = 4001, 4100, 270
     a, b = operand(1, *((k, m) if ta else (m, k)), 128 if ta else 1, gen), operand(1, *((n, k) if tb else (k, n)), 128, gen)
     compare(B.co3_matmul8(a, b, dtype=TYPES[name], transpose_a=ta, transpose_b=tb), a, b, ta, tb)
 
