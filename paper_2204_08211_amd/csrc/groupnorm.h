@@ -58,83 +58,144 @@ __device__ inline void add_pack(const Pack<_Float16, 8>::V &p, float &s, float &
     }
 }
 
-// A pack: WHOLE, all of it or (n <= 0) zeros, otherwise n values of it.
+// A thread's pack of a strip of channels c0 .. c0 + cn: V channels from `base` on, of which those from `low` up to `n` are its own; n = 0: none.  The
+// strip's last pack lies back within the pixel where it would reach beyond the strip, over channels of the pack in front, so that it is one load.
+template <int V, bool WHOLE>
+struct Lane {
+    uint32_t base;
+    int low, n;
+    __device__ inline Lane(uint32_t c0, uint32_t cn, uint32_t j, bool there)
+    {
+        const uint32_t end = c0 + cn;
+        base = c0 + j;
+        low = 0;
+        n = there && j < cn ? V : 0;
+        if (WHOLE || n == 0 || j + V <= cn) return;
+        if (end >= (uint32_t)V) {
+            low = (int)(j + V - cn);
+            base = end - V;
+        } else {
+            n = (int)(cn - j);   // a row of fewer than V channels
+        }
+    }
+    __device__ inline bool own(int k) const { return WHOLE ? n > 0 : k >= low && k < n; }
+};
+// Where channel c of a strip is among its packs' V channels each.
+template <int V>
+__device__ inline uint32_t place_of(uint32_t c0, uint32_t cn, uint32_t c) { return c < cn / V * V || c0 + cn < (uint32_t)V ? c : c + V - cn % V; }
+
+// FULL: the pixels have as many channels as a pack, or more: a pack is one load, or none.
+template <bool FULL, typename T, bool WHOLE>
+__device__ inline typename Pack<T, kVec<T>>::V load_lane(const T *row, const Lane<kVec<T>, WHOLE> &lane, bool there)
+{
+    constexpr int V = kVec<T>, H = V / 2;
+    if constexpr (FULL) {
+        return load_pack<T, V>(row, there && lane.n > 0 ? V : 0);
+    } else {
+        typename Pack<T, V>::V v;
+        const int n = there ? lane.n : 0;
+        const auto low = load_pack<T, H>(row, n), high = load_pack<T, H>(row + H, n - H);
+#pragma unroll
+        for (int k = 0; k < V; ++k) v[k] = k < H ? low[k < H ? k : 0] : high[k < H ? 0 : k - H];
+        return v;
+    }
+}
+// f(whether they are FULL), by a branch of all threads.
+template <int V, bool WHOLE, typename F>
+__device__ inline void with_rows(uint32_t channels, F &&f)
+{
+    if (WHOLE || channels >= (uint32_t)V) f(std::true_type());
+    else f(std::integral_constant<bool, WHOLE>());
+}
 template <typename T, bool WHOLE>
-__device__ inline typename Pack<T, kVec<T>>::V load_some(const T *p, int n)
+__device__ inline void store_lane(T *row, const Lane<kVec<T>, WHOLE> &lane, const typename Pack<T, kVec<T>>::V &v)
 {
     constexpr int V = kVec<T>;
-    return load_pack<T, V>(p, WHOLE ? (n > 0 ? V : 0) : n);
-}
-template <typename T, bool WHOLE>
-__device__ inline void store_some(T *p, int n, const typename Pack<T, kVec<T>>::V &v) { store_pack<T, kVec<T>>(p, WHOLE ? kVec<T> : n, v); }
-
-// red[rows][width] of a workgroup's threads -> red[q][c], q < rows left, which the return value is: sums over rows q, q + left, ...
-template <int WG>
-__device__ inline uint32_t fold_rows(float *red, uint32_t rows, uint32_t width)
-{
-    __syncthreads();
-    uint32_t left = WG / width;
-    left = left < 1 ? 1 : left < rows ? left : rows;
-    if (left < rows) {
-        for (uint32_t k = threadIdx.x; k < left * width; k += WG) {
-            const uint32_t c = k % width, q = k / width;
-            float s = red[q * width + c];
-            for (uint32_t r = q + left; r < rows; r += left) s += red[r * width + c];
-            red[q * width + c] = s;   // nobody else reads it
-        }
-        __syncthreads();
+    if (WHOLE || (lane.low == 0 && lane.n == V)) {
+        store_pack<T, V>(row, V, v);
+    } else {
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+            if (lane.own(k)) row[k] = v[k];
     }
-    return left;
 }
 
-// Sums of a workgroup's threads whose numbers are equal modulo `packs`, a power of two up to 16: red[c], c = pack V + channel, has those of
-// `s`, red[packs V + c] those of `q`.  Half of the values go to the other half of the lanes at each of two steps, so that these take
-// as many additions as there are values.
+// f(k, the group of channel k within a strip from c0 on) for the channels that are a thread's own; WHOLE: for the first, whose group is that of all.
+template <int V, bool WHOLE, typename F>
+__device__ inline void for_groups(const Lane<V, WHOLE> &lane, uint32_t c0, uint32_t per, F &&f)
+{
+    const uint32_t c = lane.base + (uint32_t)lane.low - c0;
+    uint32_t g = lane.n > 0 ? c / per : 0, r = c - g * per;
+#pragma unroll
+    for (int k = 0; k < (WHOLE ? 1 : V); ++k) {
+        if (!lane.own(k)) continue;
+        f(k, g);
+        if (++r == per) {
+            r = 0;
+            ++g;
+        }
+    }
+}
+
+// Sums of a workgroup's threads whose numbers are equal modulo `packs`, a power of two: red[c], c = pack V + channel, has those of
+// `s`, red[packs V + c] those of `q`.  Up to 16 packs a wavefront's lanes are added up first: half of the values go to the other half
+// of the lanes at each of two steps, so that these take as many additions as there are values.
 template <int V, int WG>
 __device__ inline void fold_channels(const float (&s)[V], const float (&q)[V], float *red, uint32_t packs)
 {
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x / 64, width = packs * V;
-    float t[V], u[V / 2];
-#pragma unroll
-    for (int k = 0; k < V; ++k) {   // lanes 0 to 31 go on with s, the others with q
-        const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(s[k]), __float_as_uint(q[k]), false, false);
-        t[k] = __uint_as_float(p[0]) + __uint_as_float(p[1]);
-    }
-#pragma unroll
-    for (int k = 0; k < V / 2; ++k) {   // every other sixteen lanes with the second half of the channels
-        const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(t[k]), __float_as_uint(t[k + V / 2]), false, false);
-        u[k] = __uint_as_float(p[0]) + __uint_as_float(p[1]);
-        for (uint32_t o = 8; o >= packs; o >>= 1) u[k] += __shfl_xor(u[k], o);
-    }
     float *parts = red + 2 * width;
-    if (lane % 16 < packs) {
+    uint32_t count = WG / 64;
+    if (packs <= 16) {
+        float t[V], u[V / 2];
 #pragma unroll
-        for (int k = 0; k < V / 2; ++k) parts[wave * 2 * width + lane / 32 * width + lane % 16 * V + lane / 16 % 2 * (V / 2) + k] = u[k];
+        for (int k = 0; k < V; ++k) {   // lanes 0 to 31 go on with s, the others with q
+            const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(s[k]), __float_as_uint(q[k]), false, false);
+            t[k] = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+        }
+#pragma unroll
+        for (int k = 0; k < V / 2; ++k) {   // every other sixteen lanes with the second half of the channels
+            const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(t[k]), __float_as_uint(t[k + V / 2]), false, false);
+            u[k] = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+            for (uint32_t o = 8; o >= packs; o >>= 1) u[k] += __shfl_xor(u[k], o);
+        }
+        if (lane % 16 < packs) {
+#pragma unroll
+            for (int k = 0; k < V / 2; ++k) parts[wave * 2 * width + lane / 32 * width + lane % 16 * V + lane / 16 % 2 * (V / 2) + k] = u[k];
+        }
+    } else {
+        const uint32_t row = threadIdx.x / packs, col = threadIdx.x % packs;
+        count = WG / packs;
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            parts[row * 2 * width + col * V + k] = s[k];
+            parts[row * 2 * width + width + col * V + k] = q[k];
+        }
     }
     __syncthreads();
     for (uint32_t c = threadIdx.x; c < 2 * width; c += WG) {
         float f = parts[c];
-#pragma unroll
-        for (int w = 1; w < WG / 64; ++w) f += parts[w * 2 * width + c];
+        for (uint32_t w = 1; w < count; ++w) f += parts[w * 2 * width + c];
         red[c] = f;
     }
     __syncthreads();
 }
 
-// out[g] = sum over q < rows and the group's channels of weight red[q][c]; weight may be NULL.
-template <int WG>
-__device__ inline void fold_groups(const float *red, uint32_t rows, uint32_t width, uint32_t groups, uint32_t per, const float *weight, float *out)
+// f(g, sum, sum) by one thread for every group, of what `term(place, channel)` gives of its channels: eight threads add up a group's, or a
+// wavefront where there are many.
+template <int WG, int V, typename S, typename Term, typename F>
+__device__ inline void fold_groups(uint32_t groups, uint32_t per, uint32_t c0, uint32_t cn, Term &&term, F &&f)
 {
-    for (uint32_t g = threadIdx.x / 64; g < groups; g += WG / 64) {
-        float s = 0.f;
-        for (uint32_t k = threadIdx.x % 64; k < rows * per; k += 64) {
-            const uint32_t c = g * per + k % per;
-            const float v = red[k / per * width + c];
-            s += weight ? v * weight[c] : v;
+    const uint32_t together = per > 64 ? 64 : 8;
+    for (uint32_t k = threadIdx.x; k < groups * together; k += WG) {   // those of a group go round together
+        const uint32_t g = k / together;
+        S s = 0, q = 0;
+        for (uint32_t c = g * per + k % together; c < (g + 1) * per; c += together) term(place_of<V>(c0, cn, c), c, s, q);
+        for (uint32_t o = together / 2; o; o >>= 1) {
+            s += __shfl_xor(s, o);
+            q += __shfl_xor(q, o);
         }
-#pragma unroll
-        for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o);
-        if (threadIdx.x % 64 == 0) out[g] = s;
+        if (k % together == 0) f(g, s, q);
     }
     __syncthreads();
 }
@@ -143,6 +204,15 @@ __device__ inline void fold_groups(const float *red, uint32_t rows, uint32_t wid
 struct Slices { uint32_t packs, columns, slices; };
 
 __device__ inline uint32_t slice_begin(uint32_t pixels, uint32_t slices, uint32_t i) { return (uint32_t)((uint64_t)pixels * i / slices); }
+
+// The channel at a place among a pixel's packs; one that is not there for places that another pack has.
+template <int V>
+__device__ inline uint32_t channel_at(uint32_t channels, uint32_t place)
+{
+    if (place < channels / V * V || channels < (uint32_t)V) return place;
+    const uint32_t back = V - channels % V;
+    return place % V < back ? ~0u : place - back;
+}
 
 // Two sums of all threads of a workgroup.
 template <int WG>
@@ -176,31 +246,32 @@ __host__ __device__ inline bool few_terms(uint32_t slices, uint32_t per) { retur
 
 static inline uint32_t elements_of_pack(int32_t type) { return type == CO3_F32 ? 4 : 8; }
 
-// One launch: groups of 128 bytes of a pixel or more to a workgroup, the first of the forms that holds them.  threads = 0: none does.
-struct Form { uint32_t threads, held, wide; };                          // `held` packs a thread; groups of `wide` packs of a pixel or more
-struct Whole { Strip strip; uint32_t threads, held; bool one; };       // one: packs lie within groups, and where `powers` says so are a power of two in a pixel
+// One launch: groups of `wide` packs of a pixel or more to a workgroup, the first of the forms that holds them.  threads = 0: none does.
+struct Form { uint32_t threads, held, wide; };                         // `held` packs a thread
+struct Whole { Strip strip; uint32_t threads, held, lds; bool one; };  // one: packs lie within groups
 template <size_t N>
-static Whole whole_of(uint64_t pixels, uint32_t channels, uint32_t groups, int32_t type, const Form (&forms)[N], bool powers = false)
+static Whole whole_of(uint64_t pixels, uint32_t channels, uint32_t groups, int32_t type, const Form (&forms)[N])
 {
     const uint32_t V = elements_of_pack(type), per = channels / groups;
     Whole w = {};
+    w.one = per % V == 0;
     for (const Form &f : forms) {
         w.strip.groups = (f.wide * V + per - 1) / per;
         if (w.strip.groups > groups) w.strip.groups = groups;
         w.strip.blocks = (groups + w.strip.groups - 1) / w.strip.groups;
-        w.strip.packs = (w.strip.groups * per + V - 1) / V;
-        w.one = per % V == 0 && (!powers || (w.strip.packs <= 16 && (w.strip.packs & (w.strip.packs - 1)) == 0));
+        w.strip.packs = 1;
+        while (w.strip.packs * V < w.strip.groups * per) w.strip.packs *= 2;
         if (!w.one && f.threads * f.held > 4096) continue;   // they would spill
         if (f.threads / w.strip.packs * (uint64_t)f.held < pixels) continue;
+        const uint32_t parts = w.strip.packs <= 16 ? f.threads / 64 : f.threads / w.strip.packs;
+        const uint32_t channel_sums = (1 + parts) * 2 * w.strip.packs * V, sums = channel_sums > 2 * f.threads ? channel_sums : 2 * f.threads;
+        w.lds = (sums + 2 * w.strip.groups) * (uint32_t)sizeof(float);   // of the channels, or of the threads; two numbers of every group
+        if (w.lds > 65536) continue;
         w.threads = f.threads;
         w.held = f.held;
         break;
     }
     return w;
-}
-static inline uint32_t whole_lds(const Whole &w, int32_t type)
-{
-    return (w.threads / w.strip.packs * w.strip.packs * elements_of_pack(type) + 2 * w.strip.groups) * sizeof(float);   // [rows][width], the groups' sums
 }
 
 static Slices slices_of(uint64_t samples, uint64_t pixels, uint32_t channels, int32_t type, uint64_t most_terms)

@@ -15,7 +15,8 @@ template <typename T, bool ONE> struct Source<T, false, ONE> {
     uint64_t stride;
     __device__ inline Source(const co3_groupnorm_backward_args &a, uint64_t sample, uint32_t c)
         : x(static_cast<const T *>(a.x) + sample * a.pixels * a.x_stride + c), stride(a.x_stride) { }
-    __device__ inline Raw fetch(uint32_t pixel, int n) const { return load_some<T, ONE>(x + pixel * stride, n); }
+    template <bool FULL>
+    __device__ inline Raw fetch(uint32_t pixel, const Lane<kVec<T>, ONE> &lane, bool there) const { return load_lane<FULL>(x + pixel * stride, lane, there); }
     __device__ inline typename Pack<float, kVec<T>>::V numbers(const Raw &r) const
     {
         typename Pack<float, kVec<T>>::V p;
@@ -43,8 +44,10 @@ template <typename T, bool ONE> struct Source<T, true, ONE> {
         shift = x.block_rows == 1 ? 0 : 7;
         turn = (int)(kBlockCols - c % kBlockCols);
     }
-    __device__ inline Raw fetch(uint32_t pixel, int n) const
+    template <bool FULL>
+    __device__ inline Raw fetch(uint32_t pixel, const Lane<V, ONE> &lane, bool there) const
     {
+        const int n = there ? lane.n : 0;
         Raw p;
 #pragma unroll
         for (int q = 0; q < V / 4; ++q) p.words[q] = 0;
@@ -52,7 +55,7 @@ template <typename T, bool ONE> struct Source<T, true, ONE> {
         if (n <= 0) return p;
         const uint32_t r = row + pixel;
         const uint8_t *v = values + (uint64_t)r * ld;
-        if (ONE || n >= V) {
+        if (FULL) {
             typedef uint32_t word __attribute__((aligned(1)));
 #pragma unroll
             for (int q = 0; q < V / 4; ++q) p.words[q] = reinterpret_cast<const word *>(v)[q];
@@ -84,21 +87,21 @@ template <typename T, bool ONE> struct Source<T, true, ONE> {
 template <int V, bool ONE>
 struct Channels {
     float mean[ONE ? 1 : V], rstd[ONE ? 1 : V], w[V], b[V];
-    __device__ inline void load(const co3_groupnorm_backward_args &a, uint64_t sample, uint32_t c, int n)
+    __device__ inline void load(const co3_groupnorm_backward_args &a, uint64_t sample, const Lane<V, ONE> &lane)
     {
-        const uint32_t per = a.channels / a.groups;
-#pragma unroll
-        for (int k = 0; k < (ONE ? 1 : V); ++k) {
-            const bool in = k < n;
-            const uint64_t g = sample * a.groups + (c + k) / per;
-            mean[k] = in ? a.mean[g] : 0.f;
-            rstd[k] = in ? a.rstd[g] : 0.f;
-        }
         typename Pack<float, V>::V pw, pb;
 #pragma unroll
         for (int k = 0; k < V; ++k) { pw[k] = 1.f; pb[k] = 0.f; }
-        if (a.weight) pw = load_pack<float, V>(a.weight + c, n);
-        if (a.bias) pb = load_pack<float, V>(a.bias + c, n);
+#pragma unroll
+        for (int k = 0; k < (ONE ? 1 : V); ++k) mean[k] = rstd[k] = 0.f;
+        if (lane.n > 0) {
+            for_groups(lane, 0, a.channels / a.groups, [&](int k, uint32_t g) {
+                mean[k] = a.mean[sample * a.groups + g];
+                rstd[k] = a.rstd[sample * a.groups + g];
+            });
+            if (a.weight) pw = load_pack<float, V>(a.weight + lane.base, ONE ? V : lane.n);
+            if (a.bias) pb = load_pack<float, V>(a.bias + lane.base, ONE ? V : lane.n);
+        }
 #pragma unroll
         for (int k = 0; k < V; ++k) { w[k] = pw[k]; b[k] = pb[k]; }
     }
@@ -114,25 +117,26 @@ template <typename T, bool KEPT, int ACT, int WG, int CH, bool ONE>
 __global__ __launch_bounds__(WG, 4) void k_groupnorm_backward(co3_groupnorm_backward_args a, Strip strip, uint64_t first, float *partial)
 {
     constexpr int V = kVec<T>;
-    extern __shared__ float red[];
+    extern __shared__ float sums[];   // two of every group, then what the channels' sums take
     const uint64_t sample = first + blockIdx.x;
     const uint32_t per = a.channels / a.groups, g0 = blockIdx.y * strip.groups, c0 = g0 * per;
     const uint32_t groups = a.groups - g0 < strip.groups ? a.groups - g0 : strip.groups, cn = groups * per;
-    const uint32_t rows = WG / strip.packs, width = strip.packs * V, col = threadIdx.x % strip.packs, row = threadIdx.x / strip.packs, j = col * V;
-    float *sums = red + rows * width;
-    const int n = row < rows ? (int)cn - (int)j : 0;
-    const uint32_t pixels = (uint32_t)a.pixels;
-    const uint64_t r0 = sample * a.pixels;
-    const Source<T, KEPT, ONE> source(a, sample, c0 + j);
-    const T *dy = static_cast<const T *>(a.dy) + r0 * a.dy_stride + c0 + j;
+    const uint32_t rows = WG / strip.packs, width = strip.packs * V, row = threadIdx.x / strip.packs, pixels = (uint32_t)a.pixels;
+    float *red = sums + 2 * strip.groups;
+    const Lane<V, ONE> lane(c0, cn, threadIdx.x % strip.packs * V, true);
+    const Source<T, KEPT, ONE> source(a, sample, lane.base);
+    const T *dy = static_cast<const T *>(a.dy) + sample * a.pixels * a.dy_stride + lane.base;
     typename Source<T, KEPT, ONE>::Raw raw[CH];
     typename Pack<T, V>::V d[CH];
+    with_rows<V, ONE>(a.channels, [&](auto full) {
+        constexpr bool FULL = decltype(full)::value;
 #pragma unroll
-    for (int i = 0; i < CH; ++i) raw[i] = source.fetch(row + i * rows, row + i * rows < pixels ? n : 0);
+        for (int i = 0; i < CH; ++i) raw[i] = source.template fetch<FULL>(row + i * rows, lane, row + i * rows < pixels);
 #pragma unroll
-    for (int i = 0; i < CH; ++i) d[i] = load_some<T, ONE>(dy + (row + i * rows) * a.dy_stride, row + i * rows < pixels ? n : 0);
+        for (int i = 0; i < CH; ++i) d[i] = load_lane<FULL>(dy + (row + i * rows) * a.dy_stride, lane, row + i * rows < pixels);
+    });
     Channels<V, ONE> ch;
-    ch.load(a, sample, c0 + j, n);
+    ch.load(a, sample, lane);
     float s1[V], s2[V];
 #pragma unroll
     for (int k = 0; k < V; ++k) s1[k] = s2[k] = 0.f;
@@ -147,54 +151,33 @@ __global__ __launch_bounds__(WG, 4) void k_groupnorm_backward(co3_groupnorm_back
             s2[k] = __builtin_fmaf(dz, xh, s2[k]);
         }
     }
-    if constexpr (ONE) {
-        fold_channels<V, WG>(s1, s2, red, strip.packs);   // totals of S1, then of S2
-        if (partial) {
-            for (uint32_t k = threadIdx.x; k < 2 * cn; k += WG) {
-                const uint32_t which = k / cn, c = k % cn;
-                partial[(sample * 2 + which) * a.channels + c0 + c] = red[which * width + c];
-            }
-        }
-        for (uint32_t k = threadIdx.x; k < 16 * groups; k += WG) {   // eight threads a sum: whole eights of them go round together
-            const uint32_t which = k / 8 % 2, g = k / 16;
-            float t = 0.f;
-            for (uint32_t c = k % 8; c < per; c += 8) {
-                const float v = red[which * width + g * per + c];
-                t += a.weight ? v * a.weight[c0 + g * per + c] : v;
-            }
 #pragma unroll
-            for (int o = 4; o; o >>= 1) t += __shfl_xor(t, o);
-            if (k % 8 == 0) sums[which * groups + g] = t;
+    for (int k = 0; k < V; ++k)
+        if (!lane.own(k)) s1[k] = s2[k] = 0.f;
+    fold_channels<V, WG>(s1, s2, red, strip.packs);   // totals of S1, then of S2
+    if (partial) {
+        for (uint32_t c = threadIdx.x; c < cn; c += WG) {
+            const uint32_t at = place_of<V>(c0, cn, c);
+            partial[sample * 2 * a.channels + c0 + c] = red[at];
+            partial[(sample * 2 + 1) * a.channels + c0 + c] = red[width + at];
         }
-        __syncthreads();
-    } else {
-        const auto share = [&](const float (&s)[V], float *out, uint32_t which) {
-            if (row < rows) {
-#pragma unroll
-                for (int k = 0; k < V; ++k) red[row * width + j + k] = k < n ? s[k] : 0.f;
-            }
-            const uint32_t left = fold_rows<WG>(red, rows, width);
-            if (partial) {
-                for (uint32_t c = threadIdx.x; c < cn; c += WG) {
-                    float t = red[c];
-                    for (uint32_t q = 1; q < left; ++q) t += red[q * width + c];
-                    partial[(sample * 2 + which) * a.channels + c0 + c] = t;
-                }
-            }
-            fold_groups<WG>(red, left, width, groups, per, a.weight ? a.weight + c0 : nullptr, out);
-        };
-        share(s1, sums, 0);
-        share(s2, sums + groups, 1);
     }
-    if (n <= 0) return;
+    fold_groups<WG, V, float>(groups, per, c0, cn, [&](uint32_t at, uint32_t c, float &s, float &q) {
+        const float w = a.weight ? a.weight[c0 + c] : 1.f;
+        s += w * red[at];
+        q += w * red[width + at];
+    }, [&](uint32_t g, float s, float q) {
+        sums[g] = s;
+        sums[groups + g] = q;
+    });
+    if (lane.n <= 0) return;
     const float scale = 1.f / ((float)pixels * (float)per);
-    T *dx = static_cast<T *>(a.dx) + r0 * a.dx_stride + c0 + j;
-    float m1[ONE ? 1 : V], m2[ONE ? 1 : V];
-#pragma unroll
-    for (int k = 0; k < (ONE ? 1 : V); ++k) {
-        m1[k] = k < n ? sums[(j + k) / per] * scale * ch.rstd[k] : 0.f;
-        m2[k] = k < n ? sums[groups + (j + k) / per] * scale * ch.rstd[k] : 0.f;
-    }
+    T *dx = static_cast<T *>(a.dx) + sample * a.pixels * a.dx_stride + lane.base;
+    float m1[ONE ? 1 : V] = {}, m2[ONE ? 1 : V] = {};
+    for_groups(lane, c0, per, [&](int k, uint32_t g) {
+        m1[k] = sums[g] * scale * ch.rstd[k];
+        m2[k] = sums[groups + g] * scale * ch.rstd[k];
+    });
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
         const uint32_t r = row + i * rows;
@@ -206,11 +189,30 @@ __global__ __launch_bounds__(WG, 4) void k_groupnorm_backward(co3_groupnorm_back
             const float xh = ch.xh(k, x[k]), dz = passed<ACT>((float)d[i][k], xh, ch.w[k], ch.b[k]);
             o[k] = (T)ch.dx(k, xh, dz, m1[ONE ? 0 : k], m2[ONE ? 0 : k]);
         }
-        store_some<T, ONE>(dx + r * a.dx_stride, n, o);
+        store_lane<T, ONE>(dx + r * a.dx_stride, lane, o);
     }
 }
 
 // ---- by slices of pixels ------------------------------------------------------------------------------------
+
+// red[rows][width] of a workgroup's threads -> red[q][c], q < rows left, which the return value is: sums over rows q, q + left, ...
+template <int WG>
+__device__ inline uint32_t fold_rows(float *red, uint32_t rows, uint32_t width)
+{
+    __syncthreads();
+    uint32_t left = WG / width;
+    left = left < 1 ? 1 : left < rows ? left : rows;
+    if (left < rows) {
+        for (uint32_t k = threadIdx.x; k < left * width; k += WG) {
+            const uint32_t c = k % width, q = k / width;
+            float s = red[q * width + c];
+            for (uint32_t r = q + left; r < rows; r += left) s += red[r * width + c];
+            red[q * width + c] = s;   // nobody else reads it
+        }
+        __syncthreads();
+    }
+    return left;
+}
 
 // S1 and S2 of a slice of a sample's pixels, fp32: at most 512 terms in an accumulator.
 template <typename T, bool KEPT, int ACT, bool ONE>
@@ -219,37 +221,40 @@ __global__ __launch_bounds__(256) void k_groupnorm_backward_sums(co3_groupnorm_b
     constexpr int V = kVec<T>;
     __shared__ float red[256 * V];
     const uint64_t sample = first + blockIdx.z;
-    const uint32_t rows = 256 / cut.packs, col = threadIdx.x % cut.packs, row = threadIdx.x / cut.packs, c = (blockIdx.y * cut.packs + col) * V, width = cut.packs * V;
-    const int n = row < rows ? (int)a.channels - (int)c : 0;
+    const uint32_t rows = 256 / cut.packs, col = threadIdx.x % cut.packs, row = threadIdx.x / cut.packs, width = cut.packs * V;
+    const Lane<V, ONE> lane(0, a.channels, (blockIdx.y * cut.packs + col) * V, row < rows);
     const uint32_t end = slice_begin((uint32_t)a.pixels, cut.slices, blockIdx.x + 1);
     float s1[V], s2[V];
 #pragma unroll
     for (int k = 0; k < V; ++k) s1[k] = s2[k] = 0.f;
-    if (n > 0) {
+    if (lane.n > 0) {
         Channels<V, ONE> ch;
-        ch.load(a, sample, c, n);
-        const Source<T, KEPT, ONE> source(a, sample, c);
-        const T *dy = static_cast<const T *>(a.dy) + sample * a.pixels * a.dy_stride + c;
-        for (uint32_t r = slice_begin((uint32_t)a.pixels, cut.slices, blockIdx.x) + row; r < end; r += kAtOnce * rows) {
-            typename Source<T, KEPT, ONE>::Raw raw[kAtOnce];
-            typename Pack<T, V>::V d[kAtOnce];
+        ch.load(a, sample, lane);
+        const Source<T, KEPT, ONE> source(a, sample, lane.base);
+        const T *dy = static_cast<const T *>(a.dy) + sample * a.pixels * a.dy_stride + lane.base;
+        with_rows<V, ONE>(a.channels, [&](auto full) {
+            constexpr bool FULL = decltype(full)::value;
+            for (uint32_t r = slice_begin((uint32_t)a.pixels, cut.slices, blockIdx.x) + row; r < end; r += kAtOnce * rows) {
+                typename Source<T, KEPT, ONE>::Raw raw[kAtOnce];
+                typename Pack<T, V>::V d[kAtOnce];
 #pragma unroll
-            for (int i = 0; i < kAtOnce; ++i) {
-                raw[i] = source.fetch(r + i * rows, r + i * rows < end ? n : 0);
-                d[i] = load_some<T, ONE>(dy + (r + i * rows) * a.dy_stride, r + i * rows < end ? n : 0);
-            }
+                for (int i = 0; i < kAtOnce; ++i) {
+                    raw[i] = source.template fetch<FULL>(r + i * rows, lane, r + i * rows < end);
+                    d[i] = load_lane<FULL>(dy + (r + i * rows) * a.dy_stride, lane, r + i * rows < end);
+                }
 #pragma unroll
-            for (int i = 0; i < kAtOnce; ++i) {
-                if (r + i * rows >= end) continue;
-                const auto x = source.numbers(raw[i]);
+                for (int i = 0; i < kAtOnce; ++i) {
+                    if (r + i * rows >= end) continue;
+                    const auto x = source.numbers(raw[i]);
 #pragma unroll
-                for (int k = 0; k < V; ++k) {
-                    const float xh = ch.xh(k, x[k]), dz = passed<ACT>((float)d[i][k], xh, ch.w[k], ch.b[k]);
-                    s1[k] += dz;
-                    s2[k] = __builtin_fmaf(dz, xh, s2[k]);
+                    for (int k = 0; k < V; ++k) {
+                        const float xh = ch.xh(k, x[k]), dz = passed<ACT>((float)d[i][k], xh, ch.w[k], ch.b[k]);
+                        s1[k] += dz;
+                        s2[k] = __builtin_fmaf(dz, xh, s2[k]);
+                    }
                 }
             }
-        }
+        });
     }
     float *out = partial + ((sample * cut.slices + blockIdx.x) * 2) * a.channels;
 #pragma unroll
@@ -261,7 +266,7 @@ __global__ __launch_bounds__(256) void k_groupnorm_backward_sums(co3_groupnorm_b
         }
         const uint32_t left = fold_rows<256>(red, rows, width);
         for (uint32_t k = threadIdx.x; k < width; k += 256) {
-            const uint32_t to = blockIdx.y * width + k;
+            const uint32_t to = channel_at<V>(a.channels, blockIdx.y * width + k);
             if (to >= a.channels) continue;
             float t = red[k];
             for (uint32_t q = 1; q < left; ++q) t += red[q * width + k];
@@ -275,43 +280,44 @@ __global__ __launch_bounds__(256) void k_groupnorm_backward_apply(co3_groupnorm_
 {
     constexpr int V = kVec<T>;
     const uint64_t sample = first + blockIdx.z;
-    const uint32_t rows = 256 / cut.packs, col = threadIdx.x % cut.packs, row = threadIdx.x / cut.packs, c = (blockIdx.y * cut.packs + col) * V;
-    const int n = row < rows ? (int)a.channels - (int)c : 0;
-    if (n <= 0) return;
-    const uint32_t end = slice_begin((uint32_t)a.pixels, cut.slices, blockIdx.x + 1), per = a.channels / a.groups;
+    const uint32_t rows = 256 / cut.packs, col = threadIdx.x % cut.packs, row = threadIdx.x / cut.packs;
+    const Lane<V, ONE> lane(0, a.channels, (blockIdx.y * cut.packs + col) * V, row < rows);
+    if (lane.n <= 0) return;
+    const uint32_t end = slice_begin((uint32_t)a.pixels, cut.slices, blockIdx.x + 1);
     Channels<V, ONE> ch;
-    ch.load(a, sample, c, n);
-    float m1[ONE ? 1 : V], m2[ONE ? 1 : V];
+    ch.load(a, sample, lane);
+    float m1[ONE ? 1 : V] = {}, m2[ONE ? 1 : V] = {};
+    for_groups(lane, 0, a.channels / a.groups, [&](int k, uint32_t g) {
+        m1[k] = means[2 * (sample * a.groups + g)] * ch.rstd[k];
+        m2[k] = means[2 * (sample * a.groups + g) + 1] * ch.rstd[k];
+    });
+    const Source<T, KEPT, ONE> source(a, sample, lane.base);
+    const T *dy = static_cast<const T *>(a.dy) + sample * a.pixels * a.dy_stride + lane.base;
+    T *dx = static_cast<T *>(a.dx) + sample * a.pixels * a.dx_stride + lane.base;
+    with_rows<V, ONE>(a.channels, [&](auto full) {
+        constexpr bool FULL = decltype(full)::value;
+        for (uint32_t r = slice_begin((uint32_t)a.pixels, cut.slices, blockIdx.x) + row; r < end; r += kAtOnce * rows) {
+            typename Source<T, KEPT, ONE>::Raw raw[kAtOnce];
+            typename Pack<T, V>::V d[kAtOnce];
 #pragma unroll
-    for (int k = 0; k < (ONE ? 1 : V); ++k) {
-        const uint64_t g = sample * a.groups + (c + k) / per;
-        m1[k] = k < n ? means[2 * g] * ch.rstd[k] : 0.f;
-        m2[k] = k < n ? means[2 * g + 1] * ch.rstd[k] : 0.f;
-    }
-    const Source<T, KEPT, ONE> source(a, sample, c);
-    const T *dy = static_cast<const T *>(a.dy) + sample * a.pixels * a.dy_stride + c;
-    T *dx = static_cast<T *>(a.dx) + sample * a.pixels * a.dx_stride + c;
-    for (uint32_t r = slice_begin((uint32_t)a.pixels, cut.slices, blockIdx.x) + row; r < end; r += kAtOnce * rows) {
-        typename Source<T, KEPT, ONE>::Raw raw[kAtOnce];
-        typename Pack<T, V>::V d[kAtOnce];
-#pragma unroll
-        for (int i = 0; i < kAtOnce; ++i) {
-            raw[i] = source.fetch(r + i * rows, r + i * rows < end ? n : 0);
-            d[i] = load_some<T, ONE>(dy + (r + i * rows) * a.dy_stride, r + i * rows < end ? n : 0);
-        }
-#pragma unroll
-        for (int i = 0; i < kAtOnce; ++i) {
-            if (r + i * rows >= end) continue;
-            const auto x = source.numbers(raw[i]);
-            typename Pack<T, V>::V o;
-#pragma unroll
-            for (int k = 0; k < V; ++k) {
-                const float xh = ch.xh(k, x[k]), dz = passed<ACT>((float)d[i][k], xh, ch.w[k], ch.b[k]);
-                o[k] = (T)ch.dx(k, xh, dz, m1[ONE ? 0 : k], m2[ONE ? 0 : k]);
+            for (int i = 0; i < kAtOnce; ++i) {
+                raw[i] = source.template fetch<FULL>(r + i * rows, lane, r + i * rows < end);
+                d[i] = load_lane<FULL>(dy + (r + i * rows) * a.dy_stride, lane, r + i * rows < end);
             }
-            store_some<T, ONE>(dx + (r + i * rows) * a.dx_stride, n, o);
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i) {
+                if (r + i * rows >= end) continue;
+                const auto x = source.numbers(raw[i]);
+                typename Pack<T, V>::V o;
+#pragma unroll
+                for (int k = 0; k < V; ++k) {
+                    const float xh = ch.xh(k, x[k]), dz = passed<ACT>((float)d[i][k], xh, ch.w[k], ch.b[k]);
+                    o[k] = (T)ch.dx(k, xh, dz, m1[ONE ? 0 : k], m2[ONE ? 0 : k]);
+                }
+                store_lane<T, ONE>(dx + (r + i * rows) * a.dx_stride, lane, o);
+            }
         }
-    }
+    });
 }
 
 // m1 and m2 of a group, by the threads of a wavefront or of the workgroup.
@@ -380,7 +386,7 @@ template <typename T, bool KEPT>
 static void backward_of(const co3_groupnorm_backward_args &a, hipStream_t s)
 {
     const uint64_t samples = a.U * a.samples_per_user;
-    const Whole w = whole_of(a.pixels, a.channels, a.groups, a.type, kBackward, true);
+    const Whole w = whole_of(a.pixels, a.channels, a.groups, a.type, kBackward);
     float *partial = static_cast<float *>(a.workspace), *means = nullptr;
     const uint64_t grads = a.dweight || a.dbias ? (uint64_t)a.U * ((2 * a.channels + 63) / 64) : 0;
     uint64_t parts = a.samples_per_user, others = 0;
@@ -392,7 +398,7 @@ static void backward_of(const co3_groupnorm_backward_args &a, hipStream_t s)
                 constexpr int WG = decltype(threads)::value, CH = decltype(held)::value;
                 in_parts(samples, (uint64_t)WG * w.strip.blocks, ~0ull, [&](uint64_t first, uint32_t count) {
                     k_groupnorm_backward<T, KEPT, decltype(act)::value, WG, CH, decltype(one)::value>
-                        <<<dim3(count, w.strip.blocks), dim3(WG), whole_lds(w, a.type), s>>>(a, w.strip, first, grads ? partial : nullptr);
+                        <<<dim3(count, w.strip.blocks), dim3(WG), w.lds, s>>>(a, w.strip, first, grads ? partial : nullptr);
                 });
             });
         });

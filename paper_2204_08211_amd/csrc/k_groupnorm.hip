@@ -15,27 +15,28 @@ namespace co3 {
 
 // ---- in one launch ------------------------------------------------------------------------------------------
 
-// mean and rstd of a workgroup's groups into its LDS and the caller's tensors; ONE: a pack lies within a group.
-// There the sums of x and of its squares do, in fp32 over a thread's packs and fp64 beyond, while no group's mean is more than twice its
+// mean and rstd of a workgroup's groups into its LDS.
+// The sums of x and of its squares do, in fp32 over a thread's packs and fp64 beyond, while no group's mean is more than twice its
 // spread: the variance, their difference, is off by at most five times their own 2^-23.  Otherwise the squared distances from the mean are
-// added up in a second turn, as they are where packs lie across groups.  (The packs are in registers: one turn for two is 4 us
-// of 70 us for 256 x 1024 x 256 bf16.)
+// added up in a second turn.  (The packs are in registers: one turn for two is 4 us of 66 us for 256 x 1024 x 256 bf16.)
 template <typename T, int WG, int CH, bool ONE>
 __device__ inline void statistics(const co3_groupnorm_args &a, const typename Pack<T, kVec<T>>::V (&p)[CH], float *red, float *mean, float *rstd,
-                                  uint32_t rows, uint32_t packs, uint32_t row, uint32_t col, uint32_t groups, uint32_t per, int n)
+                                  uint32_t rows, uint32_t packs, uint32_t row, uint32_t c0, uint32_t cn, uint32_t groups, uint32_t per, const Lane<kVec<T>, ONE> &lane)
 {
     constexpr int V = kVec<T>;
-    const uint32_t pixels = (uint32_t)a.pixels, j = col * V, width = packs * V;
+    const uint32_t pixels = (uint32_t)a.pixels, width = packs * V;
     const double scale = 1.0 / ((double)pixels * (double)per);
-    bool again = !ONE;
-    if constexpr (ONE) {
+    const auto decide = [&](uint32_t g, double s, double q) {
+        const double m = s * scale, var = q * scale - m * m;
+        mean[g] = (float)m;
+        rstd[g] = m * m <= 4.0 * var && var < 3e38 ? (float)(1.0 / sqrt(var + (double)a.eps)) : -1.f;
+    };
+    if constexpr (ONE) {   // a thread has one group's
         float s = 0.f, q = 0.f;
 #pragma unroll
         for (int i = 0; i < CH; ++i) add_pack(p[i], s, q);   // zeros beyond the pixels
-        if (row < rows) {
-            red[2 * threadIdx.x] = s;
-            red[2 * threadIdx.x + 1] = q;
-        }
+        red[2 * threadIdx.x] = s;
+        red[2 * threadIdx.x + 1] = q;
         __syncthreads();
         const uint32_t each = per / V;   // packs of a group in a pixel
         for (uint32_t g = threadIdx.x / 64; g < groups; g += WG / 64) {
@@ -50,89 +51,88 @@ __device__ inline void statistics(const co3_groupnorm_args &a, const typename Pa
                 ds += __shfl_xor(ds, o);
                 dq += __shfl_xor(dq, o);
             }
-            const double m = ds * scale, var = dq * scale - m * m;
-            if (threadIdx.x % 64 == 0) {
-                mean[g] = (float)m;
-                rstd[g] = m * m <= 4.0 * var && var < 3e38 ? (float)(1.0 / sqrt(var + (double)a.eps)) : -1.f;
-            }
+            if (threadIdx.x % 64 == 0) decide(g, ds, dq);
         }
         __syncthreads();
-        for (uint32_t g = 0; g < groups; ++g) again = again || rstd[g] == -1.f;
     } else {
-        float s[V];
+        float s[V], q[V];
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-            s[k] = 0.f;
+            s[k] = q[k] = 0.f;
 #pragma unroll
-            for (int i = 0; i < CH; ++i) s[k] += (float)p[i][k];
-        }
-        if (row < rows) {
-#pragma unroll
-            for (int k = 0; k < V; ++k) red[row * width + j + k] = s[k];
-        }
-        const uint32_t left = fold_rows<WG>(red, rows, width);
-        fold_groups<WG>(red, left, width, groups, per, nullptr, mean);
-        if (threadIdx.x < groups) mean[threadIdx.x] *= (float)scale;
-        __syncthreads();
-    }
-    if (again) {
-        float s[V];
-#pragma unroll
-        for (int k = 0; k < V; ++k) s[k] = 0.f;
-        if (row < rows) {
-#pragma unroll
-            for (int k = 0; k < V; ++k) {
-                if (k >= n) break;
-                const float m = mean[(j + k) / per];
-#pragma unroll
-                for (int i = 0; i < CH; ++i) {
-                    const float d = (float)p[i][k] - m;
-                    s[k] += row + i * rows < pixels ? d * d : 0.f;
-                }
+            for (int i = 0; i < CH; ++i) {
+                const float v = (float)p[i][k];
+                s[k] += v;
+                q[k] = __builtin_fmaf(v, v, q[k]);
             }
-#pragma unroll
-            for (int k = 0; k < V; ++k) red[row * width + j + k] = s[k];
+            if (!lane.own(k)) s[k] = q[k] = 0.f;
         }
-        const uint32_t left = fold_rows<WG>(red, rows, width);
-        fold_groups<WG>(red, left, width, groups, per, nullptr, rstd);
-        if (threadIdx.x < groups) rstd[threadIdx.x] = (float)(1.0 / sqrt((double)rstd[threadIdx.x] * scale + (double)a.eps));
-        __syncthreads();
+        fold_channels<V, WG>(s, q, red, packs);
+        fold_groups<WG, V, double>(groups, per, c0, cn, [&](uint32_t at, uint32_t, double &ds, double &dq) {
+            ds += red[at];
+            dq += red[width + at];
+        }, decide);
     }
+    bool again = false;
+    for (uint32_t g = 0; g < groups; ++g) again = again || rstd[g] == -1.f;
+    if (!again) return;
+    float s[V], none[V], m[ONE ? 1 : V] = {};
+    for_groups(lane, c0, per, [&](int k, uint32_t g) { m[k] = mean[g]; });
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+        s[k] = none[k] = 0.f;
+        if (!lane.own(k)) continue;
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            const float v = (float)p[i][k] - m[ONE ? 0 : k];
+            s[k] += row + i * rows < pixels ? v * v : 0.f;
+        }
+    }
+    __syncthreads();   // all have seen that
+    fold_channels<V, WG>(s, none, red, packs);
+    fold_groups<WG, V, double>(groups, per, c0, cn, [&](uint32_t at, uint32_t, double &ds, double &) { ds += red[at]; },
+                               [&](uint32_t g, double ds, double) { rstd[g] = (float)(1.0 / sqrt(ds * scale + (double)a.eps)); });
 }
 
 template <typename T, int ACT, int WG, int CH, bool ONE>
 __global__ __launch_bounds__(WG, 4) void k_groupnorm(co3_groupnorm_args a, Strip strip, uint64_t first)
 {
     constexpr int V = kVec<T>;
-    extern __shared__ float red[];   // [rows][packs V], then the groups' mean and rstd
+    extern __shared__ float red[];   // the groups' mean and rstd, then what the sums take
     const uint64_t sample = first + blockIdx.x;
     const uint32_t per = a.channels / a.groups, g0 = blockIdx.y * strip.groups, c0 = g0 * per;
     const uint32_t groups = a.groups - g0 < strip.groups ? a.groups - g0 : strip.groups, cn = groups * per;
-    const uint32_t rows = WG / strip.packs, col = threadIdx.x % strip.packs, row = threadIdx.x / strip.packs, j = col * V;
-    float *mean = red + rows * strip.packs * V, *rstd = mean + strip.groups;
-    const int n = row < rows ? (int)cn - (int)j : 0;
-    const uint32_t pixels = (uint32_t)a.pixels;
-    const T *x = static_cast<const T *>(a.x) + sample * a.pixels * a.x_stride + c0 + j;
+    const uint32_t rows = WG / strip.packs, row = threadIdx.x / strip.packs, pixels = (uint32_t)a.pixels;
+    float *mean = red, *rstd = mean + strip.groups;
+    const Lane<V, ONE> lane(c0, cn, threadIdx.x % strip.packs * V, true);
+    const T *x = static_cast<const T *>(a.x) + sample * a.pixels * a.x_stride + lane.base;
     typename Pack<T, V>::V p[CH];
+    with_rows<V, ONE>(a.channels, [&](auto full) {
 #pragma unroll
-    for (int i = 0; i < CH; ++i) p[i] = load_some<T, ONE>(x + (row + i * rows) * a.x_stride, row + i * rows < pixels ? n : 0);
-    statistics<T, WG, CH, ONE>(a, p, red, mean, rstd, rows, strip.packs, row, col, groups, per, n);
+        for (int i = 0; i < CH; ++i) p[i] = load_lane<decltype(full)::value>(x + (row + i * rows) * a.x_stride, lane, row + i * rows < pixels);
+    });
+    statistics<T, WG, CH, ONE>(a, p, red + 2 * strip.groups, mean, rstd, rows, strip.packs, row, c0, cn, groups, per, lane);
     if (threadIdx.x < groups) {
         const uint64_t at = sample * a.groups + g0 + threadIdx.x;
         if (a.mean) a.mean[at] = mean[threadIdx.x];
         if (a.rstd) a.rstd[at] = rstd[threadIdx.x];
     }
-    if (n <= 0) return;
-    float m[ONE ? 1 : V], f[V], b[V];
+    if (lane.n <= 0) return;
+    float m[ONE ? 1 : V] = {}, f[V], b[V];
+    typename Pack<float, V>::V w, add;
 #pragma unroll
-    for (int k = 0; k < V; ++k) {
-        const bool in = k < n;
-        if (!ONE || k == 0) m[k] = in ? mean[(j + k) / per] : 0.f;
-        const float r = in ? rstd[(j + (ONE ? 0 : k)) / per] : 0.f;
-        f[k] = in && a.weight ? r * a.weight[c0 + j + k] : r;
-        b[k] = in && a.bias ? a.bias[c0 + j + k] : 0.f;
-    }
-    T *y = static_cast<T *>(a.y) + sample * a.pixels * a.y_stride + c0 + j;
+    for (int k = 0; k < V; ++k) { w[k] = 1.f; add[k] = 0.f; }
+    if (a.weight) w = load_pack<float, V>(a.weight + lane.base, ONE ? V : lane.n);
+    if (a.bias) add = load_pack<float, V>(a.bias + lane.base, ONE ? V : lane.n);
+#pragma unroll
+    for (int k = 0; k < V; ++k) { f[k] = 0.f; b[k] = add[k]; }
+    for_groups(lane, c0, per, [&](int k, uint32_t g) {
+        m[k] = mean[g];
+        f[k] = rstd[g];
+    });
+#pragma unroll
+    for (int k = V - 1; k >= 0; --k) f[k] = f[ONE ? 0 : k] * w[k];
+    T *y = static_cast<T *>(a.y) + sample * a.pixels * a.y_stride + lane.base;
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
         const uint32_t r = row + i * rows;
@@ -140,7 +140,7 @@ __global__ __launch_bounds__(WG, 4) void k_groupnorm(co3_groupnorm_args a, Strip
         typename Pack<T, V>::V o;
 #pragma unroll
         for (int k = 0; k < V; ++k) o[k] = (T)activated<ACT>(__builtin_fmaf((float)p[i][k] - m[ONE ? 0 : k], f[k], b[k]));
-        store_some<T, ONE>(y + r * a.y_stride, n, o);
+        store_lane<T, ONE>(y + r * a.y_stride, lane, o);
     }
 }
 
@@ -153,27 +153,29 @@ __global__ __launch_bounds__(256) void k_groupnorm_sums(co3_groupnorm_args a, Sl
     constexpr int V = kVec<T>;
     __shared__ double red[256 * V];
     const uint64_t sample = first + blockIdx.z;
-    const uint32_t rows = 256 / cut.packs, col = threadIdx.x % cut.packs, row = threadIdx.x / cut.packs, c = (blockIdx.y * cut.packs + col) * V, width = cut.packs * V;
-    const int n = row < rows ? (int)a.channels - (int)c : 0;
+    const uint32_t rows = 256 / cut.packs, col = threadIdx.x % cut.packs, row = threadIdx.x / cut.packs, width = cut.packs * V;
+    const Lane<V, false> lane(0, a.channels, (blockIdx.y * cut.packs + col) * V, row < rows);
     const uint32_t end = slice_begin((uint32_t)a.pixels, cut.slices, blockIdx.x + 1);
-    const T *x = static_cast<const T *>(a.x) + sample * a.pixels * a.x_stride + c;
+    const T *x = static_cast<const T *>(a.x) + sample * a.pixels * a.x_stride + lane.base;
     double s[V], q[V];
 #pragma unroll
     for (int k = 0; k < V; ++k) s[k] = q[k] = 0.0;
-    if (n > 0) {
-        for (uint32_t r = slice_begin((uint32_t)a.pixels, cut.slices, blockIdx.x) + row; r < end; r += kAtOnce * rows) {
-            typename Pack<T, V>::V p[kAtOnce];
+    if (lane.n > 0) {
+        with_rows<V, false>(a.channels, [&](auto full) {
+            for (uint32_t r = slice_begin((uint32_t)a.pixels, cut.slices, blockIdx.x) + row; r < end; r += kAtOnce * rows) {
+                typename Pack<T, V>::V p[kAtOnce];
 #pragma unroll
-            for (int i = 0; i < kAtOnce; ++i) p[i] = load_pack<T, V>(x + (r + i * rows) * a.x_stride, r + i * rows < end ? n : 0);
+                for (int i = 0; i < kAtOnce; ++i) p[i] = load_lane<decltype(full)::value>(x + (r + i * rows) * a.x_stride, lane, r + i * rows < end);
 #pragma unroll
-            for (int i = 0; i < kAtOnce; ++i)
+                for (int i = 0; i < kAtOnce; ++i)
 #pragma unroll
-                for (int k = 0; k < V; ++k) {
-                    const double v = (double)(float)p[i][k];
-                    s[k] += v;
-                    q[k] = __builtin_fma(v, v, q[k]);
-                }
-        }
+                    for (int k = 0; k < V; ++k) {
+                        const double v = (double)(float)p[i][k];
+                        s[k] += v;
+                        q[k] = __builtin_fma(v, v, q[k]);
+                    }
+            }
+        });
     }
     double *out = partial + ((sample * cut.slices + blockIdx.x) * 2) * a.channels;
 #pragma unroll
@@ -185,7 +187,7 @@ __global__ __launch_bounds__(256) void k_groupnorm_sums(co3_groupnorm_args a, Sl
         }
         __syncthreads();
         for (uint32_t k = threadIdx.x; k < width; k += 256) {
-            const uint32_t to = blockIdx.y * width + k;
+            const uint32_t to = channel_at<V>(a.channels, blockIdx.y * width + k);
             if (to >= a.channels) continue;
             double t = red[k];
             for (uint32_t r = 1; r < rows; ++r) t += red[r * width + k];
@@ -219,34 +221,39 @@ __global__ __launch_bounds__(256) void k_groupnorm_apply(co3_groupnorm_args a, S
 {
     constexpr int V = kVec<T>;
     const uint64_t sample = first + blockIdx.z;
-    const uint32_t rows = 256 / cut.packs, col = threadIdx.x % cut.packs, row = threadIdx.x / cut.packs, c = (blockIdx.y * cut.packs + col) * V;
-    const int n = row < rows ? (int)a.channels - (int)c : 0;
-    if (n <= 0) return;
+    const uint32_t rows = 256 / cut.packs, col = threadIdx.x % cut.packs, row = threadIdx.x / cut.packs;
+    const Lane<V, false> lane(0, a.channels, (blockIdx.y * cut.packs + col) * V, row < rows);
+    if (lane.n <= 0) return;
     const uint32_t end = slice_begin((uint32_t)a.pixels, cut.slices, blockIdx.x + 1), per = a.channels / a.groups;
     float m[V], f[V], b[V];
+    typename Pack<float, V>::V w, add;
 #pragma unroll
-    for (int k = 0; k < V; ++k) {
-        const bool in = k < n;
-        const uint64_t g = sample * a.groups + (c + k) / per;
-        m[k] = in ? mean[g] : 0.f;
-        f[k] = in ? (a.weight ? rstd[g] * a.weight[c + k] : rstd[g]) : 0.f;
-        b[k] = in && a.bias ? a.bias[c + k] : 0.f;
-    }
-    const T *x = static_cast<const T *>(a.x) + sample * a.pixels * a.x_stride + c;
-    T *y = static_cast<T *>(a.y) + sample * a.pixels * a.y_stride + c;
-    for (uint32_t r = slice_begin((uint32_t)a.pixels, cut.slices, blockIdx.x) + row; r < end; r += kAtOnce * rows) {
-        typename Pack<T, V>::V p[kAtOnce];
+    for (int k = 0; k < V; ++k) { m[k] = f[k] = 0.f; w[k] = 1.f; add[k] = 0.f; }
+    if (a.weight) w = load_pack<float, V>(a.weight + lane.base, lane.n);
+    if (a.bias) add = load_pack<float, V>(a.bias + lane.base, lane.n);
+    for_groups(lane, 0, per, [&](int k, uint32_t g) {
+        m[k] = mean[sample * a.groups + g];
+        f[k] = rstd[sample * a.groups + g];
+    });
 #pragma unroll
-        for (int i = 0; i < kAtOnce; ++i) p[i] = load_pack<T, V>(x + (r + i * rows) * a.x_stride, r + i * rows < end ? n : 0);
+    for (int k = 0; k < V; ++k) { f[k] *= w[k]; b[k] = add[k]; }
+    const T *x = static_cast<const T *>(a.x) + sample * a.pixels * a.x_stride + lane.base;
+    T *y = static_cast<T *>(a.y) + sample * a.pixels * a.y_stride + lane.base;
+    with_rows<V, false>(a.channels, [&](auto full) {
+        for (uint32_t r = slice_begin((uint32_t)a.pixels, cut.slices, blockIdx.x) + row; r < end; r += kAtOnce * rows) {
+            typename Pack<T, V>::V p[kAtOnce];
 #pragma unroll
-        for (int i = 0; i < kAtOnce; ++i) {
-            if (r + i * rows >= end) continue;
-            typename Pack<T, V>::V o;
+            for (int i = 0; i < kAtOnce; ++i) p[i] = load_lane<decltype(full)::value>(x + (r + i * rows) * a.x_stride, lane, r + i * rows < end);
 #pragma unroll
-            for (int k = 0; k < V; ++k) o[k] = (T)activated<ACT>(__builtin_fmaf((float)p[i][k] - m[k], f[k], b[k]));
-            store_pack<T, V>(y + (r + i * rows) * a.y_stride, n, o);
+            for (int i = 0; i < kAtOnce; ++i) {
+                if (r + i * rows >= end) continue;
+                typename Pack<T, V>::V o;
+#pragma unroll
+                for (int k = 0; k < V; ++k) o[k] = (T)activated<ACT>(__builtin_fmaf((float)p[i][k] - m[k], f[k], b[k]));
+                store_lane<T, false>(y + (r + i * rows) * a.y_stride, lane, o);
+            }
         }
-    }
+    });
 }
 
 // ---- launches -----------------------------------------------------------------------------------------------
@@ -262,7 +269,7 @@ size_t groupnorm_backward_workspace_bytes(uint32_t U, uint64_t samples_per_user,
 {
     const uint64_t samples = U * samples_per_user;
     if (samples == 0) return 0;
-    if (whole_of(pixels, channels, groups, type, kBackward, true).threads) return samples * 2 * channels * sizeof(float);
+    if (whole_of(pixels, channels, groups, type, kBackward).threads) return samples * 2 * channels * sizeof(float);
     const Slices c = slices_of(samples, pixels, channels, type, kMostTerms);
     return up16(samples * c.slices * 2 * channels * sizeof(float)) + samples * groups * 2 * sizeof(float);
 }
@@ -278,7 +285,7 @@ static void forward_of(const co3_groupnorm_args &a, hipStream_t s)
                 constexpr int WG = decltype(threads)::value, CH = decltype(held)::value;
                 in_parts(a.samples, (uint64_t)WG * w.strip.blocks, ~0ull, [&](uint64_t first, uint32_t count) {
                     k_groupnorm<T, decltype(act)::value, WG, CH, decltype(one)::value>
-                        <<<dim3(count, w.strip.blocks), dim3(WG), whole_lds(w, a.type), s>>>(a, w.strip, first);
+                        <<<dim3(count, w.strip.blocks), dim3(WG), w.lds, s>>>(a, w.strip, first);
                 });
             });
         });
