@@ -10,9 +10,12 @@ own data, and the PS updates its matrices as Muon does.  One iteration, all of i
           a plain step (--sgd: the matrices too)                                       (line 14)
 
 The network is h <- h + W2 relu(W1 norm(h)) a few times and out = W norm(h), fitted to a fixed random network of the same kind.
+With --images it is one for images, in 8 bits: h <- h + W n a few times and out = W n, n = silu(group norm(h)), at every pixel.  Its
+products are co3_matmul8's, of tensors that co3_quantize8 makes; what the backward pass needs, h and n of every block, is kept as
+such a tensor, a byte an element.
 Prints the mean squared error and the bits per element sent.
 
-    python -m paper_2204_08211_amd.examples.local_training [--users 4] [--width 256] [--blocks 3] [--iters 100] [--sgd]
+    python -m paper_2204_08211_amd.examples.local_training [--users 4] [--width 256] [--blocks 3] [--iters 100] [--sgd STEP] [--images PIXELS]
 """
 import argparse
 import math
@@ -22,15 +25,10 @@ import torch
 from paper_2204_08211_amd import binding as B
 
 
-class Network:
-    """The layout of the model in its flat vector, and both passes for all users at once."""
+class Layout:
+    """The layout of a model in its flat vector."""
 
-    def __init__(self, width, hidden, blocks, outputs):
-        self.width, self.blocks = width, blocks
-        shapes = []
-        for k in range(blocks):
-            shapes += [(f"weight{k}", (width,)), (f"bias{k}", (width,)), (f"up{k}", (hidden, width)), (f"down{k}", (width, hidden))]
-        shapes += [("weight_out", (width,)), ("bias_out", (width,)), ("out", (outputs, width))]
+    def __init__(self, shapes):
         self.at, offset = {}, 0
         for name, shape in shapes:
             self.at[name] = (offset, shape)
@@ -57,6 +55,17 @@ class Network:
         o, shape = self.at[name]
         return flat[..., o:o + math.prod(shape)].unflatten(-1, shape) if len(shape) == 2 else flat[..., o:o + shape[0]]
 
+
+class Network(Layout):
+    """Both passes for all users at once."""
+
+    def __init__(self, width, hidden, blocks, outputs):
+        self.width, self.blocks = width, blocks
+        shapes = []
+        for k in range(blocks):
+            shapes += [(f"weight{k}", (width,)), (f"bias{k}", (width,)), (f"up{k}", (hidden, width)), (f"down{k}", (width, hidden))]
+        super().__init__(shapes + [("weight_out", (width,)), ("bias_out", (width,)), ("out", (outputs, width))])
+
     def forward(self, w, x):
         """Outputs for x [users, rows, width], and what the backward pass needs."""
         kept, h = [], x
@@ -82,6 +91,46 @@ class Network:
             self.part(g, f"up{k}").copy_(da.mT.contiguous() @ n)
             dh = dh + B.co3_layernorm_backward(da @ self.part(w, f"up{k}"), h, self.part(w, f"weight{k}"), mean, rstd,
                                                dweight=self.part(g, f"weight{k}"), dbias=self.part(g, f"bias{k}"))
+
+
+class ImageNetwork(Layout):
+    """The same for images of `pixels` pixels, rows / pixels of them a user, with group norms, products and what is kept in 8 bits."""
+
+    def __init__(self, width, blocks, outputs, pixels, groups=8):
+        self.width, self.blocks, self.pixels, self.groups = width, blocks, pixels, groups
+        shapes = []
+        for k in range(blocks):
+            shapes += [(f"weight{k}", (width,)), (f"bias{k}", (width,)), (f"mix{k}", (width, width))]
+        super().__init__(shapes + [("weight_out", (width,)), ("bias_out", (width,)), ("out", (outputs, width))])
+
+    def _layer(self, w, h, name, matrix, kept, dtype):
+        """matrix silu(group norm(h)) of h [users, rows, width]."""
+        n, mean, rstd = B.co3_groupnorm(h.view(-1, self.pixels, self.width), self.groups, self.part(w, f"weight{name}"), self.part(w, f"bias{name}"),
+                                        activation=B.ACT_SILU)
+        n8, w8 = B.co3_quantize8(n.view(h.shape)), B.co3_quantize8(self.part(w, matrix))
+        kept.append((B.co3_quantize8(h), n8, w8, mean, rstd))
+        return B.co3_matmul8(n8, w8, dtype=dtype, transpose_b=True)
+
+    def _layer_backward(self, w, dy, name, matrix, kept, g):
+        """The gradient of h, and the layer's into every user's row of g."""
+        h8, n8, w8, mean, rstd = kept
+        dy8 = B.co3_quantize8(dy)
+        B.co3_matmul8(dy8, n8, out=self.part(g, matrix), transpose_a=True)
+        dn = B.co3_matmul8(dy8, w8)
+        dh = B.co3_groupnorm_backward(dn.view(-1, self.pixels, self.width), h8, self.groups, self.part(w, f"weight{name}"), self.part(w, f"bias{name}"), mean, rstd,
+                                      activation=B.ACT_SILU, users=dn.shape[0], dweight=self.part(g, f"weight{name}"), dbias=self.part(g, f"bias{name}"))
+        return dh.view(dn.shape)
+
+    def forward(self, w, x):
+        kept, h = [], x.bfloat16()
+        for k in range(self.blocks):
+            h = h + self._layer(w, h, k, f"mix{k}", kept, torch.bfloat16)
+        return self._layer(w, h, "_out", "out", kept, torch.float32), kept
+
+    def backward(self, w, dy, kept, g):
+        dh = self._layer_backward(w, dy, "_out", "out", kept[-1], g)
+        for k in reversed(range(self.blocks)):
+            dh = dh + self._layer_backward(w, dh, k, f"mix{k}", kept[k], g)
 
 
 def train(net, users=4, rows=256, iters=100, eta=0.02, eta_vectors=0.5, gamma=0.7, refresh=10, sgd=None, E=4, M=3, seed=1, device="cuda:0"):
@@ -135,8 +184,9 @@ def main():
     p.add_argument("--iters", type=int, default=100)
     p.add_argument("--eta", type=float, default=0.02)
     p.add_argument("--sgd", type=float, default=None, help="plain updates of this step instead")
+    p.add_argument("--images", type=int, default=None, help="images of so many pixels (a divisor of --rows), in 8 bits")
     a = p.parse_args()
-    net = Network(a.width, a.hidden, a.blocks, a.outputs)
+    net = Network(a.width, a.hidden, a.blocks, a.outputs) if a.images is None else ImageNetwork(a.width, a.blocks, a.outputs, a.images)
     errors, bits = train(net, a.users, a.rows, a.iters, a.eta, sgd=a.sgd)
     print(f"U={a.users} d={net.d} {'orthogonalised updates' if a.sgd is None else 'plain updates'}: mean squared error "
           + ", ".join(f"{errors[t]:.4f} at {t}" for t in sorted({0, a.iters // 4, a.iters // 2, a.iters - 1})) + f"; {bits:.3f} bit/element")
