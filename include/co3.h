@@ -460,7 +460,7 @@ int co3_layernorm_backward(const co3_layernorm_backward_args *args, void *stream
 
 /* ---- activations and products in 8 bits ---------------------------------------------------
  * Matrices of e4m3 numbers (a sign, 4 bits of an exponent, 3 of a fraction, no infinities) with a power of two as the scale of
- * each block of 128 columns by block_rows rows, 128 or 1; x = value 2^(scale - 127).  Blocks of 128 rows can be read along
+ * each block of 128 columns by block_rows rows, 128 or 1; x = value 2^(scale - 127), scales are 1 to 254.  Blocks of 128 rows can be read along
  * either side: one copy of an activation serves the forward product, waits for the backward pass in a byte an element, and
  * serves the weight's gradient there.  Every matrix of a batch has blocks of its own.
  * The bytes of a row from cols up to the next multiple of 16 are zeros (co3_quantize8 writes them).                     */
@@ -508,9 +508,10 @@ int co3_dequantize8(const co3_dequantize8_args *args, void *stream);
  * W [outputs][inputs], dx = dy W and, for every user, dW = dy^T x: `out` may be a layer's part of the users' gradients that
  * co3_encode reads.  Where the sum runs along the rows (a transposed, b not) the blocks have 128 rows.
  * Sums are fp32 and rounded once.  Results of 16 bits are made by the matrix instructions for 8-bit numbers, which add sixteen
- * products at a time, cut off at some 2^-16 of the largest (2e-5 to 7e-5 of the result, a hundredth of its rounding to bf16); those
+ * products at a time, cut off at some 2^-16 of the largest (measured 1e-5 to 8e-5 of the result; its rounding to bf16 is 1.7e-3); those
  * of fp32 by the instructions for bf16, in which these numbers, and their products in fp32, are exact (numbers below 2^-126 may count
- * as zeros there).  k = 0 gives zeros.
+ * as zeros there).  k = 0 gives zeros.  out may not lie where a or b does.
+ * CO3_ERR_CAPACITY: more than 2^22 tiles of a matrix, of 16 rows by 16 columns where m <= 16, or too small a workspace.
  * workspace: device, co3_matmul8_workspace_bytes() of these args, 16-byte aligned; NULL where that is 0.                */
 typedef struct {
     co3_blocks8 a, b;

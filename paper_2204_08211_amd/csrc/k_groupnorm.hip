@@ -6,9 +6,14 @@
 //            dx = rstd (dz w - m1 - xh m2),  dweight[u] = sum over the user's samples of S2,  dbias[u] = of S1
 // so one pass over the data gives all sums, and a second one dx.
 //
-// Two ways.  Where a workgroup can hold a sample's pixels of some whole groups (128 bytes of a pixel or more) in registers, it reads them once
+// Two ways.  Where a workgroup can hold a sample's pixels of some whole groups (64 or 128 bytes of a pixel, or more) in registers, it reads them once
 // and all is one launch.  Beyond that the sums of slices of pixels go through the workspace, and x (and dy) are read twice.
 // All sums are formed in a fixed order.
+//
+// Measured (MI355X, a large copy runs at 4.8 TB/s; kernels): forward 256 x 1024 x 256 bf16 with SiLU 63 to 68 us = 4.3 to 3.9 TB/s; 8 x 16384 x 256 by slices
+// 22 + 5 + 23 us.  Backward of 128 x 1024 x 256 bf16 from x in 8 bits 59 us with SiLU, where vector instructions fill 72 % of the cycles (dz is made twice,
+// since the registers hold x and dy), 48 without an activation; 5 more for the users' gradients.  4 x 16384 x 512 by slices 38 + 6 + 34 us.
+// Groups of 15 channels, 128 x 1024 x 60 fp32, by slices 14 + 4.5 + 17 us (41 + 5 in one launch, of partial packs).
 #include "groupnorm.h"
 
 namespace co3 {
@@ -18,7 +23,7 @@ namespace co3 {
 // mean and rstd of a workgroup's groups into its LDS.
 // The sums of x and of its squares do, in fp32 over a thread's packs and fp64 beyond, while no group's mean is more than twice its
 // spread: the variance, their difference, is off by at most five times their own 2^-23.  Otherwise the squared distances from the mean are
-// added up in a second turn.  (The packs are in registers: one turn for two is 4 us of 66 us for 256 x 1024 x 256 bf16.)
+// added up in a second turn.
 template <typename T, int WG, int CH, bool ONE>
 __device__ inline void statistics(const co3_groupnorm_args &a, const typename Pack<T, kVec<T>>::V (&p)[CH], float *red, float *mean, float *rstd,
                                   uint32_t rows, uint32_t packs, uint32_t row, uint32_t c0, uint32_t cn, uint32_t groups, uint32_t per, const Lane<kVec<T>, ONE> &lane)
