@@ -298,7 +298,7 @@ constexpr uint64_t kNoLimit = 1ull << 31, kMostTerms = 512;
 template <typename F>
 static void in_parts(uint64_t count, uint64_t threads, uint64_t at_once, F &&launch)
 {
-    const uint64_t room = ((1ull << 32) - 1) / threads, most = room < at_once ? room : at_once;
+    const uint64_t room = ((1ull << 32) - 1) / threads, most = room == 0 ? 1 : room < at_once ? room : at_once;   // 0: a launch that is refused
     for (uint64_t i = 0; i < count; i += most) launch(i, (uint32_t)(count - i < most ? count - i : most));
 }
 

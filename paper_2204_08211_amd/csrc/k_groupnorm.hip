@@ -23,7 +23,7 @@ namespace co3 {
 // mean and rstd of a workgroup's groups into its LDS.
 // The sums of x and of its squares do, in fp32 over a thread's packs and fp64 beyond, while no group's mean is more than twice its
 // spread: the variance, their difference, is off by at most five times their own 2^-23.  Otherwise the squared distances from the mean are
-// added up in a second turn.
+// added up in a second turn, and where squares leave fp32 at either end, of x times a power of two, which rounds nothing.
 template <typename T, int WG, int CH, bool ONE>
 __device__ inline void statistics(const co3_groupnorm_args &a, const typename Pack<T, kVec<T>>::V (&p)[CH], float *red, float *mean, float *rstd,
                                   uint32_t rows, uint32_t packs, uint32_t row, uint32_t c0, uint32_t cn, uint32_t groups, uint32_t per, const Lane<kVec<T>, ONE> &lane)
@@ -33,8 +33,9 @@ __device__ inline void statistics(const co3_groupnorm_args &a, const typename Pa
     const double scale = 1.0 / ((double)pixels * (double)per);
     const auto decide = [&](uint32_t g, double s, double q) {
         const double m = s * scale, var = q * scale - m * m;
+        const bool large = !(q < 1e37), small = q * scale < 1e-24 && a.eps < 1e-17f;   // large: also what is not finite
         mean[g] = (float)m;
-        rstd[g] = m * m <= 4.0 * var && var < 3e38 ? (float)(1.0 / sqrt(var + (double)a.eps)) : -1.f;
+        rstd[g] = large ? -0x1p-80f : small ? -0x1p80f : m * m <= 4.0 * var ? (float)(1.0 / sqrt(var + (double)a.eps)) : -1.f;   // below 0: the power of two
     };
     if constexpr (ONE) {   // a thread has one group's
         float s = 0.f, q = 0.f;
@@ -78,10 +79,28 @@ __device__ inline void statistics(const co3_groupnorm_args &a, const typename Pa
             dq += red[width + at];
         }, decide);
     }
-    bool again = false;
-    for (uint32_t g = 0; g < groups; ++g) again = again || rstd[g] == -1.f;
+    bool again = false, large = false;
+    for (uint32_t g = 0; g < groups; ++g) {
+        again = again || rstd[g] < 0.f;
+        large = large || rstd[g] == -0x1p-80f;
+    }
     if (!again) return;
-    float s[V], none[V], m[ONE ? 1 : V] = {};
+    const auto power = [&](uint32_t g) { return rstd[g] < 0.f ? -rstd[g] : 1.f; };
+    float s[V], none[V], m[ONE ? 1 : V] = {}, f[ONE ? 1 : V] = {};
+    for_groups(lane, c0, per, [&](int k, uint32_t g) { f[k] = power(g); });
+    __syncthreads();   // all have seen the groups'
+    if (large) {       // their sums may have left fp32 too
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            s[k] = none[k] = 0.f;
+            if (!lane.own(k)) continue;
+#pragma unroll
+            for (int i = 0; i < CH; ++i) s[k] += (float)p[i][k] * f[ONE ? 0 : k];   // zeros beyond the pixels
+        }
+        fold_channels<V, WG>(s, none, red, packs);
+        fold_groups<WG, V, double>(groups, per, c0, cn, [&](uint32_t at, uint32_t, double &ds, double &) { ds += red[at]; },
+                                   [&](uint32_t g, double ds, double) { mean[g] = rstd[g] == -0x1p-80f ? (float)(ds * scale * 0x1p80) : mean[g]; });
+    }
     for_groups(lane, c0, per, [&](int k, uint32_t g) { m[k] = mean[g]; });
 #pragma unroll
     for (int k = 0; k < V; ++k) {
@@ -89,14 +108,15 @@ __device__ inline void statistics(const co3_groupnorm_args &a, const typename Pa
         if (!lane.own(k)) continue;
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
-            const float v = (float)p[i][k] - m[ONE ? 0 : k];
+            const float v = __builtin_fmaf((float)p[i][k], f[ONE ? 0 : k], -m[ONE ? 0 : k] * f[ONE ? 0 : k]);
             s[k] += row + i * rows < pixels ? v * v : 0.f;
         }
     }
-    __syncthreads();   // all have seen that
     fold_channels<V, WG>(s, none, red, packs);
-    fold_groups<WG, V, double>(groups, per, c0, cn, [&](uint32_t at, uint32_t, double &ds, double &) { ds += red[at]; },
-                               [&](uint32_t g, double ds, double) { rstd[g] = (float)(1.0 / sqrt(ds * scale + (double)a.eps)); });
+    fold_groups<WG, V, double>(groups, per, c0, cn, [&](uint32_t at, uint32_t, double &ds, double &) { ds += red[at]; }, [&](uint32_t g, double ds, double) {
+        const double t = power(g);
+        rstd[g] = (float)(1.0 / sqrt(ds * scale / (t * t) + (double)a.eps));
+    });
 }
 
 template <typename T, int ACT, int WG, int CH, bool ONE>
