@@ -1,4 +1,4 @@
-// Host side of the operators in 8 bits declared in include/co3.h: argument checks, how a product is cut into workgroups.
+// Host side of the operators in 8 bits and of group norm declared in include/co3.h: argument checks, how a product is cut into workgroups.
 #include <algorithm>
 #include <cmath>
 
@@ -116,6 +116,13 @@ size_t workspace_of(const Matmul8Plan &p)
     return p.slices > 1 ? (size_t)p.slices * p.batch * p.m * p.part_ld * sizeof(float) : 0;
 }
 
+inline bool valid_activation(int32_t t) { return t == CO3_ACT_NONE || t == CO3_ACT_RELU || t == CO3_ACT_SILU; }
+inline bool valid_groups(uint64_t samples, uint64_t pixels, uint32_t channels, uint32_t groups, int32_t type)
+{
+    if (!valid_type(type) || channels == 0 || channels > CO3_MAX_NORM_COLS || groups == 0 || channels % groups) return false;
+    return pixels != 0 && pixels < (1ull << 31) && samples < (1ull << 31) && samples * pixels < (1ull << 31);
+}
+
 }  // namespace
 
 extern "C" {
@@ -156,6 +163,66 @@ int co3_matmul8(const co3_matmul8_args *a, void *stream)
         if (a->workspace_bytes < need) return CO3_ERR_CAPACITY;
     }
     return launch_matmul8(*a, p, static_cast<hipStream_t>(stream)) == hipSuccess ? CO3_OK : CO3_ERR_HIP;
+}
+
+size_t co3_groupnorm_workspace_bytes(uint64_t samples, uint64_t pixels, uint32_t channels, uint32_t groups, int32_t type)
+{
+    return valid_groups(samples, pixels, channels, groups, type) ? groupnorm_workspace_bytes(samples, pixels, channels, groups, type) : 0;
+}
+
+int co3_groupnorm(const co3_groupnorm_args *a, void *stream)
+{
+    if (!a || !valid_groups(a->samples, a->pixels, a->channels, a->groups, a->type) || !valid_activation(a->activation)) return CO3_ERR_ARG;
+    if (!(a->eps >= 0.f) || std::isinf(a->eps)) return CO3_ERR_ARG;
+    if (a->samples == 0) return CO3_OK;
+    const size_t size = type_bytes(a->type);
+    if (!a->x || !a->y || !aligned(a->x, size) || !aligned(a->y, size)) return CO3_ERR_ARG;
+    if (!aligned(a->weight, 4) || !aligned(a->bias, 4) || !aligned(a->mean, 4) || !aligned(a->rstd, 4)) return CO3_ERR_ARG;
+    if (a->x_stride < a->channels || a->y_stride < a->channels || a->x_stride > kMostStride || a->y_stride > kMostStride) return CO3_ERR_ARG;
+    if (a->x == a->y && a->x_stride != a->y_stride) return CO3_ERR_ARG;
+    if (const size_t need = groupnorm_workspace_bytes(a->samples, a->pixels, a->channels, a->groups, a->type); need) {
+        if (!a->workspace || !aligned(a->workspace, 16)) return CO3_ERR_ARG;
+        if (a->workspace_bytes < need) return CO3_ERR_CAPACITY;
+    }
+    return launch_groupnorm(*a, static_cast<hipStream_t>(stream)) == hipSuccess ? CO3_OK : CO3_ERR_HIP;
+}
+
+size_t co3_groupnorm_backward_workspace_bytes(uint32_t U, uint64_t samples_per_user, uint64_t pixels, uint32_t channels, uint32_t groups, int32_t type)
+{
+    if (U == 0 || U > 65535u || samples_per_user >= (1ull << 31) || !valid_groups(U * samples_per_user, pixels, channels, groups, type)) return 0;
+    return groupnorm_backward_workspace_bytes(U, samples_per_user, pixels, channels, groups, type);
+}
+
+int co3_groupnorm_backward(const co3_groupnorm_backward_args *a, void *stream)
+{
+    if (!a || a->U == 0 || a->U > 65535u || a->samples_per_user >= (1ull << 31) || !valid_activation(a->activation)) return CO3_ERR_ARG;
+    const uint64_t samples = a->U * a->samples_per_user;
+    if (!valid_groups(samples, a->pixels, a->channels, a->groups, a->type)) return CO3_ERR_ARG;
+    const size_t size = type_bytes(a->type);
+    const bool grads = a->dweight || a->dbias;
+    if (!aligned(a->weight, 4) || !aligned(a->bias, 4) || !aligned(a->mean, 4) || !aligned(a->rstd, 4) || !aligned(a->dweight, 4) || !aligned(a->dbias, 4))
+        return CO3_ERR_ARG;
+    if (grads && a->U > 1 && (a->grad_stride < a->channels || a->grad_stride > kMostStride)) return CO3_ERR_ARG;
+    if (samples) {
+        if (!a->dy || !a->dx || !a->mean || !a->rstd || !aligned(a->dy, size) || !aligned(a->dx, size)) return CO3_ERR_ARG;
+        if (a->dy_stride < a->channels || a->dx_stride < a->channels || a->dy_stride > kMostStride || a->dx_stride > kMostStride) return CO3_ERR_ARG;
+        if (a->dx == a->dy && a->dx_stride != a->dy_stride) return CO3_ERR_ARG;
+        if (a->x) {
+            if (!aligned(a->x, size) || a->x_stride < a->channels || a->x_stride > kMostStride || (a->dx == a->x && a->dx_stride != a->x_stride)) return CO3_ERR_ARG;
+        } else {
+            if (!valid_blocks8(a->x8) || a->x8.cols != a->channels || (a->x8.batch != 1 && a->x8.batch != a->U) ||
+                a->x8.rows * a->x8.batch != samples * a->pixels)
+                return CO3_ERR_ARG;
+        }
+    } else if (!grads) {
+        return CO3_OK;
+    }
+    const size_t need = groupnorm_backward_workspace_bytes(a->U, a->samples_per_user, a->pixels, a->channels, a->groups, a->type);
+    if (need) {
+        if (!a->workspace || !aligned(a->workspace, 16)) return CO3_ERR_ARG;
+        if (a->workspace_bytes < need) return CO3_ERR_CAPACITY;
+    }
+    return launch_groupnorm_backward(*a, static_cast<hipStream_t>(stream)) == hipSuccess ? CO3_OK : CO3_ERR_HIP;
 }
 
 }  // extern "C"
