@@ -463,6 +463,7 @@ int co3_layernorm_backward(const co3_layernorm_backward_args *args, void *stream
  * each block of 128 columns by block_rows rows, 128 or 1; x = value 2^(scale - 127), scales are 1 to 254.  Blocks of 128 rows can be read along
  * either side: one copy of an activation serves the forward product, waits for the backward pass in a byte an element, and
  * serves the weight's gradient there.  Every matrix of a batch has blocks of its own.
+ * A workspace belongs to one call until that has ended on its stream: calls that may overlap, graphs among them, take one each.
  * The bytes of a row from cols up to the next multiple of 16 are zeros (co3_quantize8 writes them).                     */
 typedef struct {
     uint8_t *values;         /* device, 16-byte aligned: row r of matrix i begins at byte i batch_stride + r ld         */

@@ -34,6 +34,7 @@ inline bool aligned(const void *p, size_t n) { return (reinterpret_cast<uintptr_
 inline uint32_t up(uint32_t x, uint32_t n) { return (x + n - 1) / n * n; }
 inline size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 inline bool valid_type(int32_t t) { return t == CO3_F32 || t == CO3_BF16 || t == CO3_F16; }
+
 constexpr uint32_t kMaxMatrices = 65536, kMaxSide = 1u << 20;
 constexpr uint64_t kMostThreads = (1ull << 32) - 1;   // of a launch: workgroups of 1024 threads at most for tiles, of 256 for norms and layout
 constexpr uint64_t kMaxTiles = kMostThreads / 1024, kMaxParts = kMostThreads / 256;
