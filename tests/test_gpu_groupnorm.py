@@ -339,3 +339,21 @@ def test_other_streams_and_a_replayed_graph(pixels):
         step()
         assert all(torch.equal(p, q) for p, q in zip(got, outs))
     assert all(torch.equal(p, q) for p, q in zip(first, outs))
+
+
+@pytest.mark.parametrize("pixels", [60, 1500])     # in one launch, and by slices
+def test_offsets_beyond_32_bits(pixels):
+    """Pixels 2^22 elements apart, more than 2^32 in all: the bits of the same call on pixels next to each other."""
+    from paper_2204_08211_amd import binding as B
+    far, n, c = 1 << 22, -(-1500 // pixels), 30
+    x, dy, weight, bias = make(n, pixels, c, 5, torch.bfloat16, 7, "silu")
+    at = [torch.empty(n * pixels * far, dtype=torch.bfloat16, device="cuda:0").as_strided((n, pixels, c), (pixels * far, far, 1)) for _ in range(4)]
+    at[0].copy_(x)
+    at[1].copy_(dy)
+    y, mean, rstd = B.co3_groupnorm(x, 5, weight, bias, activation=B.ACT_SILU)
+    far_y, far_mean, far_rstd = B.co3_groupnorm(at[0], 5, weight, bias, activation=B.ACT_SILU, y=at[2])
+    assert torch.equal(far_y, y) and torch.equal(far_mean, mean) and torch.equal(far_rstd, rstd)
+    grads, far_grads = torch.zeros(2, 1, c, device="cuda:0"), torch.zeros(2, 1, c, device="cuda:0")
+    dx = B.co3_groupnorm_backward(dy, x, 5, weight, bias, mean, rstd, activation=B.ACT_SILU, dweight=grads[0], dbias=grads[1])
+    far_dx = B.co3_groupnorm_backward(at[1], at[0], 5, weight, bias, mean, rstd, activation=B.ACT_SILU, dx=at[3], dweight=far_grads[0], dbias=far_grads[1])
+    assert torch.equal(far_dx, dx) and torch.equal(far_grads, grads)

@@ -208,3 +208,31 @@ def test_other_streams_and_a_replayed_graph():
         step()
         assert torch.equal(got[0], dx) and torch.equal(got[1], dw) and not torch.equal(got[1], first[1])
         compare(dw, dy, x, True, False)
+
+
+@pytest.mark.parametrize("ta,tb", FORMS)
+@pytest.mark.parametrize("m", [7, 300])     # few rows, and tiles
+def test_offsets_beyond_32_bits(m, ta, tb):
+    """Rows 2^22 bytes and elements apart, 1100 and more of them: the bits of the same product of rows next to each other."""
+    from paper_2204_08211_amd import binding as B
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(m)
+    far, k, n = 1 << 22, 1100, 1100
+    shape = (1, n, 130) if tb else (1, k, 130)
+    x = torch.randn(shape, generator=gen, device="cuda:0").bfloat16()
+    near = B.co3_quantize8(x)
+    apart = torch.empty(shape[1] * far, dtype=torch.bfloat16, device="cuda:0").as_strided(shape, (0, far, 1))
+    apart.copy_(x)
+    values = torch.empty(shape[1] * far, dtype=torch.uint8, device="cuda:0").as_strided((1, shape[1], 144), (shape[1] * far, far, 1))
+    b = B.Blocks8(values, torch.empty_like(near.scales), 130)
+    B.co3_quantize8(apart, out=b)
+    assert torch.equal(b.values, near.values) and torch.equal(b.scales[:, :, :9], near.scales[:, :, :9])
+    assert torch.equal(B.co3_dequantize8(b), B.co3_dequantize8(near))
+    inner = 130 if tb else k
+    a = B.co3_quantize8(torch.randn((1, inner, m) if ta else (1, m, inner), generator=gen, device="cuda:0"))
+    want = B.co3_matmul8(a, near, transpose_a=ta, transpose_b=tb)
+    assert torch.equal(B.co3_matmul8(a, b, transpose_a=ta, transpose_b=tb), want)
+    # b in the place of the first operand, results far apart
+    c = B.co3_quantize8(torch.randn(1, 40, 130, generator=gen, device="cuda:0"))
+    out = torch.empty(shape[1] * far, dtype=torch.bfloat16, device="cuda:0").as_strided((1, shape[1], 40), (0, far, 1))
+    assert torch.equal(B.co3_matmul8(b, c, out=out, transpose_b=True), B.co3_matmul8(near, c, transpose_b=True))
