@@ -525,7 +525,7 @@ typedef struct {
     void *workspace;
     size_t workspace_bytes;
 } co3_matmul8_args;
-size_t co3_matmul8_workspace_bytes(const co3_matmul8_args *args);   /* 0 for args that co3_matmul8 refuses; out and workspace are not looked at */
+size_t co3_matmul8_workspace_bytes(const co3_matmul8_args *args);   /* the type of out counts; 0 for args that co3_matmul8 refuses; out and workspace are not looked at */
 int co3_matmul8(const co3_matmul8_args *args, void *stream);
 
 /* Group norm with an activation, channels last: pixel p of sample i is row i pixels + p.  Over the pixels and the channels

@@ -928,8 +928,10 @@ def co3_dequantize8(x, out=None, dtype=None, stream=None):
     return out
 
 
-def co3_matmul8_workspace_bytes(a, b, transpose_a=False, transpose_b=False):
-    return int(lib().co3_matmul8_workspace_bytes(_pack_matmul8(*a._fields, *b._fields, 0, 0, 0, F32, bool(transpose_a), bool(transpose_b), 0, 0, 0)))
+def co3_matmul8_workspace_bytes(a, b, transpose_a=False, transpose_b=False, dtype=None):
+    """Bytes for a result of `dtype`, which has a part in how a product is cut; where none is given, for one of any type."""
+    size, kinds = lib().co3_matmul8_workspace_bytes, (F32, BF16, F16) if dtype is None else (tensor_type(dtype),)
+    return max(int(size(_pack_matmul8(*a._fields, *b._fields, 0, 0, 0, kind, 1 if transpose_a else 0, 1 if transpose_b else 0, 0, 0, 0))) for kind in kinds)
 
 
 def co3_matmul8(a, b, out=None, dtype=None, transpose_a=False, transpose_b=False, accumulate=False, workspace=None, stream=None):
@@ -953,7 +955,7 @@ def co3_matmul8(a, b, out=None, dtype=None, transpose_a=False, transpose_b=False
             if out is None:
                 out = torch.empty((batch, m, n), dtype=torch.bfloat16 if dtype is None else dtype, device=a.values.device)
             if workspace is None:
-                workspace = torch.empty(co3_matmul8_workspace_bytes(a, b, transpose_a, transpose_b), dtype=torch.uint8, device=a.values.device)
+                workspace = torch.empty(co3_matmul8_workspace_bytes(a, b, transpose_a, transpose_b, out.dtype), dtype=torch.uint8, device=a.values.device)
     out_batch, rows, cols, stride, between = _matrices(out, "out")
     if out_batch != batch or rows != m or cols != n or out.get_device() != a.gpu:
         raise ValueError(f"out: [{batch}, {m}, {n}] on the device of a is taken")
