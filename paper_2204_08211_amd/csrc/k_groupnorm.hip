@@ -21,9 +21,12 @@ namespace co3 {
 // ---- in one launch ------------------------------------------------------------------------------------------
 
 // mean and rstd of a workgroup's groups into its LDS.
-// The sums of x and of its squares do, in fp32 over a thread's packs and fp64 beyond, while no group's mean is more than twice its
-// spread: the variance, their difference, is off by at most five times their own 2^-23.  Otherwise the squared distances from the mean are
-// added up in a second turn, and where squares leave fp32 at either end, of x times a power of two, which rounds nothing.
+// The sums of x and of its squares do while no group's mean is more than twice its spread: formed in fp32 over a thread's packs (of partial ones
+// over the workgroup's threads too), with at most 128 terms one behind the other, and in fp64 beyond, each is off by at most 128 2^-24 of its
+// terms' sizes, and the variance, their difference, by five times that.  Otherwise the distances from the mean, and their squares, are
+// added up in a second turn, and where squares leave fp32 at either end, those of x times a power of two, which rounds nothing.  That mean
+// is an fp32 number near the group's, off by e; the distances' mean says how far, and its square leaves the variance: off by at most 32 2^-24 (1 + 2 (e / spread)^2)
+// of itself, whatever the mean.
 template <typename T, int WG, int CH, bool ONE>
 __device__ inline void statistics(const co3_groupnorm_args &a, const typename Pack<T, kVec<T>>::V (&p)[CH], float *red, float *mean, float *rstd,
                                   uint32_t rows, uint32_t packs, uint32_t row, uint32_t c0, uint32_t cn, uint32_t groups, uint32_t per, const Lane<kVec<T>, ONE> &lane)
@@ -102,20 +105,26 @@ __device__ inline void statistics(const co3_groupnorm_args &a, const typename Pa
                                    [&](uint32_t g, double ds, double) { mean[g] = rstd[g] == -0x1p-80f ? (float)(ds * scale * 0x1p80) : mean[g]; });
     }
     for_groups(lane, c0, per, [&](int k, uint32_t g) { m[k] = mean[g]; });
+    float off[V];
 #pragma unroll
     for (int k = 0; k < V; ++k) {
-        s[k] = none[k] = 0.f;
+        s[k] = off[k] = 0.f;
         if (!lane.own(k)) continue;
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
-            const float v = __builtin_fmaf((float)p[i][k], f[ONE ? 0 : k], -m[ONE ? 0 : k] * f[ONE ? 0 : k]);
-            s[k] += row + i * rows < pixels ? v * v : 0.f;
+            const float v = __builtin_fmaf((float)p[i][k], f[ONE ? 0 : k], -m[ONE ? 0 : k] * f[ONE ? 0 : k]), d = row + i * rows < pixels ? v : 0.f;
+            s[k] = __builtin_fmaf(d, d, s[k]);
+            off[k] += d;
         }
     }
-    fold_channels<V, WG>(s, none, red, packs);
-    fold_groups<WG, V, double>(groups, per, c0, cn, [&](uint32_t at, uint32_t, double &ds, double &) { ds += red[at]; }, [&](uint32_t g, double ds, double) {
-        const double t = power(g);
-        rstd[g] = (float)(1.0 / sqrt(ds * scale / (t * t) + (double)a.eps));
+    fold_channels<V, WG>(s, off, red, packs);
+    fold_groups<WG, V, double>(groups, per, c0, cn, [&](uint32_t at, uint32_t, double &ds, double &dd) {
+        ds += red[at];
+        dd += red[width + at];
+    }, [&](uint32_t g, double ds, double dd) {
+        const double t = power(g), e = dd * scale, var = ds * scale - e * e;
+        if (fabs(e) < INFINITY) mean[g] = (float)((double)mean[g] + e / t);   // an infinite mean stays
+        rstd[g] = (float)(1.0 / sqrt((var > 0.0 ? var : var != var ? var : 0.0) / (t * t) + (double)a.eps));
     });
 }
 
