@@ -180,34 +180,60 @@ __global__ __launch_bounds__(WG, 4) void k_groupnorm(co3_groupnorm_args a, Strip
 
 // ---- by slices of pixels ------------------------------------------------------------------------------------
 
-// Sums of x and of its squares, in fp64: no mean harms the variance, and no finite fp32 input overflows.
-template <typename T>
+// What a group's distances are taken from: its first value, or 0 where that is not finite.
+__device__ inline float taken_from(float first) { return fabsf(first) < INFINITY ? first : 0.f; }
+
+// Those of a thread's channels (WHOLE: of the first).  All loads before the first one is looked at, without a branch between them.
+template <typename T, bool WHOLE>
+__device__ inline void first_values(const T *sample, uint32_t per, const Lane<kVec<T>, WHOLE> &lane, float *from)
+{
+    constexpr int N = WHOLE ? 1 : kVec<T>;
+    const uint32_t c = lane.n > 0 ? lane.base : 0;
+    uint32_t g = c / per, r = c - g * per;
+    T v[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        v[k] = sample[k < lane.n ? g * per : 0];
+        r = r + 1 == per ? 0 : r + 1;
+        g += r == 0 ? 1 : 0;
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k) from[k] = taken_from((float)v[k]);
+}
+
+// Sums of the distances from a value of the group, and of their squares, in fp64, where no finite input overflows.  Any of n values is at most
+// sqrt(n) times the spread away from the mean, so whatever the mean is, the variance, a difference, is off by some n 2^-53 of itself at most.
+template <typename T, bool ONE>
 __global__ __launch_bounds__(256) void k_groupnorm_sums(co3_groupnorm_args a, Slices cut, uint64_t first, double *partial)
 {
     constexpr int V = kVec<T>;
     __shared__ double red[256 * V];
     const uint64_t sample = first + blockIdx.z;
     const uint32_t rows = 256 / cut.packs, col = threadIdx.x % cut.packs, row = threadIdx.x / cut.packs, width = cut.packs * V;
-    const Lane<V, false> lane(0, a.channels, (blockIdx.y * cut.packs + col) * V, row < rows);
-    const uint32_t end = slice_begin((uint32_t)a.pixels, cut.slices, blockIdx.x + 1);
-    const T *x = static_cast<const T *>(a.x) + sample * a.pixels * a.x_stride + lane.base;
+    const Lane<V, ONE> lane(0, a.channels, (blockIdx.y * cut.packs + col) * V, row < rows);
+    const uint32_t end = slice_begin((uint32_t)a.pixels, cut.slices, blockIdx.x + 1), per = a.channels / a.groups;
+    const T *all = static_cast<const T *>(a.x) + sample * a.pixels * a.x_stride, *x = all + lane.base;
     double s[V], q[V];
+    float from[ONE ? 1 : V];
+    first_values(all, per, lane, from);
 #pragma unroll
     for (int k = 0; k < V; ++k) s[k] = q[k] = 0.0;
     if (lane.n > 0) {
-        with_rows<V, false>(a.channels, [&](auto full) {
+        with_rows<V, ONE>(a.channels, [&](auto full) {
             for (uint32_t r = slice_begin((uint32_t)a.pixels, cut.slices, blockIdx.x) + row; r < end; r += kAtOnce * rows) {
                 typename Pack<T, V>::V p[kAtOnce];
 #pragma unroll
                 for (int i = 0; i < kAtOnce; ++i) p[i] = load_lane<decltype(full)::value>(x + (r + i * rows) * a.x_stride, lane, r + i * rows < end);
 #pragma unroll
-                for (int i = 0; i < kAtOnce; ++i)
+                for (int i = 0; i < kAtOnce; ++i) {
+                    if (r + i * rows >= end) continue;
 #pragma unroll
                     for (int k = 0; k < V; ++k) {
-                        const double v = (double)(float)p[i][k];
+                        const double v = (double)(float)p[i][k] - (double)from[ONE ? 0 : k];
                         s[k] += v;
                         q[k] = __builtin_fma(v, v, q[k]);
                     }
+                }
             }
         });
     }
@@ -231,7 +257,7 @@ __global__ __launch_bounds__(256) void k_groupnorm_sums(co3_groupnorm_args a, Sl
 }
 
 // mean and rstd of a group, a workgroup each: of one wavefront where there is little to add up, otherwise of sixteen.
-template <int WG>
+template <typename T, int WG>
 __global__ __launch_bounds__(WG) void k_groupnorm_stats(co3_groupnorm_args a, uint32_t slices, uint64_t first, const double *partial, float *mean, float *rstd)
 {
     const uint64_t k = first + blockIdx.x, sample = k / a.groups;
@@ -246,7 +272,7 @@ __global__ __launch_bounds__(WG) void k_groupnorm_stats(co3_groupnorm_args a, ui
     fold_two<WG>(s, q);
     if (threadIdx.x) return;
     const double n = 1.0 / ((double)a.pixels * per), m = s * n, var = q * n - m * m;
-    mean[k] = (float)m;
+    mean[k] = (float)((double)taken_from((float)static_cast<const T *>(a.x)[sample * a.pixels * a.x_stride + c0]) + m);
     rstd[k] = (float)(1.0 / sqrt((var > 0.0 ? var : var != var ? var : 0.0) + (double)a.eps));
 }
 
@@ -332,12 +358,14 @@ static void forward_of(const co3_groupnorm_args &a, hipStream_t s)
     {
         ProfScope prof(K_GROUPNORM_SUMS, s);
         in_parts(a.samples, (uint64_t)256 * c.slices * c.columns, 65535, [&](uint64_t first, uint32_t count) {
-            k_groupnorm_sums<T><<<dim3(c.slices, c.columns, count), dim3(256), 0, s>>>(a, c, first, partial);
+            const dim3 grid(c.slices, c.columns, count);
+            if (w.one) k_groupnorm_sums<T, true><<<grid, dim3(256), 0, s>>>(a, c, first, partial);
+            else k_groupnorm_sums<T, false><<<grid, dim3(256), 0, s>>>(a, c, first, partial);
         });
         const bool few = few_terms(c.slices, a.channels / a.groups);
         in_parts(a.samples * a.groups, few ? 64 : 1024, ~0ull, [&](uint64_t first, uint32_t count) {
-            if (few) k_groupnorm_stats<64><<<dim3(count), dim3(64), 0, s>>>(a, c.slices, first, partial, mean, rstd);
-            else k_groupnorm_stats<1024><<<dim3(count), dim3(1024), 0, s>>>(a, c.slices, first, partial, mean, rstd);
+            if (few) k_groupnorm_stats<T, 64><<<dim3(count), dim3(64), 0, s>>>(a, c.slices, first, partial, mean, rstd);
+            else k_groupnorm_stats<T, 1024><<<dim3(count), dim3(1024), 0, s>>>(a, c.slices, first, partial, mean, rstd);
         });
     }
     ProfScope prof(K_GROUPNORM, s);

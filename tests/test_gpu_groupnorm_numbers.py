@@ -1,18 +1,18 @@
 """Group norm's statistics where a group's mean is far larger than its spread, where values are infinite or small (pytest -m gpu).
 
-Tolerance of rstd.  The squared distances are taken from a mean m that is off by at most T 2^-25 |mean|, T the fp32 terms one
+Tolerance of rstd.  In one launch the squared distances are taken from a mean m that is off by at most T 2^-25 |mean|, T the fp32 terms one
 behind the other in its sums, 64 at most, and the mean distance's square is taken off again.  Distances are exact here, and their sums,
 whole multiples of the values' step below 2^24 of them, too; squares' sums are of multiples of the step's square and exact
 as well while below 2^24.  What is left are fp64's roundings and rstd's own, 2^-24, and where sums of squares pass 2^24 steps at most 32 roundings of
 2^-24 of a sum that is (1 + (m's error / spread)^2) times the variance, here at most 5 times: 160 2^-24 of the variance, 80 2^-24 < 2^-17 of rstd.
-The mean's tolerance is half its step for its sums and one for what they are rounded to: 2^-23."""
+By slices everything is fp64, off by far less.  The mean's tolerance is half its step for fp64 sums and one for what they are rounded to: 2^-23."""
 import pytest
 import torch
 
 pytestmark = pytest.mark.gpu
 
-# pixels, channels, groups: whole packs, partial ones, one and sixteen packs a thread
-SIZES = [(1, 64, 1), (50, 16, 2), (50, 15, 5), (256, 64, 8), (1000, 64, 8), (1024, 256, 32), (9, 2048, 1)]
+# pixels, channels, groups: one launch of whole packs, of partial ones, of one and of sixteen packs a thread; by slices
+SIZES = [(1, 64, 1), (50, 16, 2), (50, 15, 5), (256, 64, 8), (1000, 64, 8), (1024, 256, 32), (700, 30, 5), (20000, 16, 2), (20000, 15, 5), (9, 2048, 1)]
 
 
 def statistics(x, groups, eps):
@@ -25,6 +25,7 @@ def statistics(x, groups, eps):
 @pytest.mark.parametrize("steps", [3, 28, 1000])     # the mean is some 2^23, 2^20, 2^15 times the spread
 @pytest.mark.parametrize("pixels,channels,groups", SIZES)
 def test_means_far_larger_than_the_spread(pixels, channels, groups, steps):
+    """The same rstd whatever way the size takes."""
     from paper_2204_08211_amd import binding as B
     gen = torch.Generator(device="cuda:0")
     gen.manual_seed(pixels + channels + steps)
