@@ -556,6 +556,7 @@ int co3_groupnorm(const co3_groupnorm_args *args, void *stream);
 /* Its backward pass for U users of samples_per_user samples each:
  *   xh = (x - mean) rstd,  z = xh weight + bias,  dz = dy act'(z),  t = dz weight,  dx = rstd (t - mean(t) - xh mean(t xh)), the means
  *   over the group;  dweight[u] = sum over the user's pixels of dz xh,  dbias[u] = sum of dz, in a fixed order.
+ * ReLU's z is rounded as in co3_groupnorm: from the same x, mean and rstd, what was let through has a gradient and nothing else.
  * x is given in `type`, or (x NULL) in 8 bits, x8: `batch` = U matrices of samples_per_user pixels rows, or one of all.
  * dweight, dbias, grad_stride, accumulate as in co3_layernorm_backward.  dx may be dy or x.                             */
 typedef struct {

@@ -152,20 +152,18 @@ __global__ __launch_bounds__(WG, 4) void k_groupnorm(co3_groupnorm_args a, Strip
         if (a.rstd) a.rstd[at] = rstd[threadIdx.x];
     }
     if (lane.n <= 0) return;
-    float m[ONE ? 1 : V] = {}, f[V], b[V];
-    typename Pack<float, V>::V w, add;
+    float m[ONE ? 1 : V] = {}, f[ONE ? 1 : V] = {};
+    typename Pack<float, V>::V w, b;
 #pragma unroll
-    for (int k = 0; k < V; ++k) { w[k] = 1.f; add[k] = 0.f; }
+    for (int k = 0; k < V; ++k) { w[k] = 1.f; b[k] = 0.f; }
     if (a.weight) w = load_pack<float, V>(a.weight + lane.base, ONE ? V : lane.n);
-    if (a.bias) add = load_pack<float, V>(a.bias + lane.base, ONE ? V : lane.n);
-#pragma unroll
-    for (int k = 0; k < V; ++k) { f[k] = 0.f; b[k] = add[k]; }
+    if (a.bias) b = load_pack<float, V>(a.bias + lane.base, ONE ? V : lane.n);
     for_groups(lane, c0, per, [&](int k, uint32_t g) {
         m[k] = mean[g];
         f[k] = rstd[g];
     });
-#pragma unroll
-    for (int k = V - 1; k >= 0; --k) f[k] = f[ONE ? 0 : k] * w[k];
+    arrived<V>(w);
+    arrived<V>(b);
     T *y = static_cast<T *>(a.y) + sample * a.pixels * a.y_stride + lane.base;
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
@@ -173,7 +171,7 @@ __global__ __launch_bounds__(WG, 4) void k_groupnorm(co3_groupnorm_args a, Strip
         if (r >= pixels) continue;
         typename Pack<T, V>::V o;
 #pragma unroll
-        for (int k = 0; k < V; ++k) o[k] = (T)activated<ACT>(__builtin_fmaf((float)p[i][k] - m[ONE ? 0 : k], f[k], b[k]));
+        for (int k = 0; k < V; ++k) o[k] = (T)activated<ACT>(argument<ACT>((float)p[i][k], m[ONE ? 0 : k], f[ONE ? 0 : k], w[k], b[k]));
         store_lane<T, ONE>(y + r * a.y_stride, lane, o);
     }
 }
@@ -285,18 +283,16 @@ __global__ __launch_bounds__(256) void k_groupnorm_apply(co3_groupnorm_args a, S
     const Lane<V, false> lane(0, a.channels, (blockIdx.y * cut.packs + col) * V, row < rows);
     if (lane.n <= 0) return;
     const uint32_t end = slice_begin((uint32_t)a.pixels, cut.slices, blockIdx.x + 1), per = a.channels / a.groups;
-    float m[V], f[V], b[V];
-    typename Pack<float, V>::V w, add;
+    float m[V], f[V];
+    typename Pack<float, V>::V w, b;
 #pragma unroll
-    for (int k = 0; k < V; ++k) { m[k] = f[k] = 0.f; w[k] = 1.f; add[k] = 0.f; }
+    for (int k = 0; k < V; ++k) { m[k] = f[k] = 0.f; w[k] = 1.f; b[k] = 0.f; }
     if (a.weight) w = load_pack<float, V>(a.weight + lane.base, lane.n);
-    if (a.bias) add = load_pack<float, V>(a.bias + lane.base, lane.n);
+    if (a.bias) b = load_pack<float, V>(a.bias + lane.base, lane.n);
     for_groups(lane, 0, per, [&](int k, uint32_t g) {
         m[k] = mean[sample * a.groups + g];
         f[k] = rstd[sample * a.groups + g];
     });
-#pragma unroll
-    for (int k = 0; k < V; ++k) { f[k] *= w[k]; b[k] = add[k]; }
     const T *x = static_cast<const T *>(a.x) + sample * a.pixels * a.x_stride + lane.base;
     T *y = static_cast<T *>(a.y) + sample * a.pixels * a.y_stride + lane.base;
     with_rows<V, false>(a.channels, [&](auto full) {
@@ -309,7 +305,7 @@ __global__ __launch_bounds__(256) void k_groupnorm_apply(co3_groupnorm_args a, S
                 if (r + i * rows >= end) continue;
                 typename Pack<T, V>::V o;
 #pragma unroll
-                for (int k = 0; k < V; ++k) o[k] = (T)activated<ACT>(__builtin_fmaf((float)p[i][k] - m[k], f[k], b[k]));
+                for (int k = 0; k < V; ++k) o[k] = (T)activated<ACT>(argument<ACT>((float)p[i][k], m[k], f[k], w[k], b[k]));
                 store_lane<T, false>(y + (r + i * rows) * a.y_stride, lane, o);
             }
         }
