@@ -182,3 +182,27 @@ def test_training_on_images_repeats_itself():
     again, _ = train(net, users=3, rows=256, iters=6)
     assert all(e == e and e < 1e3 for e in errors) and 1.0 < bits < 9.0
     assert errors[:1] == again[:1] and all(abs(a - b) <= 1e-3 * a for a, b in zip(errors, again))
+
+
+@pytest.mark.parametrize("images", [True, False])
+def test_training_gives_the_same_bits(images):
+    """All sums are formed in a fixed order, the codec's and the update's too: another run has the same errors and sends as many bits."""
+    from paper_2204_08211_amd.examples.local_training import ImageNetwork, Network, train
+    net = ImageNetwork(64, 2, 16, 64) if images else Network(64, 128, 2, 16)
+    assert train(net, users=3, rows=256, iters=6) == train(net, users=3, rows=256, iters=6)
+
+
+def test_the_networks_gradients_have_the_same_bits():
+    from paper_2204_08211_amd.examples.local_training import ImageNetwork
+    net = ImageNetwork(64, 2, 16, 64)
+    w = net.start(3, "cuda:0")
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(9)
+    x, dy = (torch.randn(3, 1024, n, generator=gen, device="cuda:0") for n in (64, 16))
+    first = None
+    for _ in range(8):
+        g = torch.zeros(3, net.d, device="cuda:0")
+        out, kept = net.forward(w, x)
+        net.backward(w, dy, kept, g)
+        first = (out, g) if first is None else first
+        assert torch.equal(out, first[0]) and torch.equal(g, first[1])
