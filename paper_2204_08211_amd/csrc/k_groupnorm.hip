@@ -11,7 +11,7 @@
 // All sums are formed in a fixed order.
 //
 // Measured (MI355X, a large copy runs at 4.8 TB/s; kernels): forward 256 x 1024 x 256 bf16 with SiLU 63 to 68 us = 4.3 to 3.9 TB/s; 8 x 16384 x 256 by slices
-// 22 + 5 + 23 us.  Backward of 128 x 1024 x 256 bf16 from x in 8 bits 59 us with SiLU, where vector instructions fill 72 % of the cycles (dz is made twice,
+// 22 + 6 + 24 us.  Backward of 128 x 1024 x 256 bf16 from x in 8 bits 59 us with SiLU, where vector instructions fill 72 % of the cycles (dz is made twice,
 // since the registers hold x and dy), 48 without an activation; 5 more for the users' gradients.  4 x 16384 x 512 by slices 38 + 6 + 34 us.
 // Groups of 15 channels, 128 x 1024 x 60 fp32, by slices 14 + 4.5 + 17 us (41 + 5 in one launch, of partial packs).
 #include "groupnorm.h"

@@ -12,7 +12,7 @@
 // the sums fp32's (1e-7), at half of the rate.
 //
 // Measured (MI355X, normal numbers; the library's product of 8192 x 8192 e4m3 numbers with one scale 2.81 PFLOP/s, of bf16 1.54): 8192 x 4096 x 4096
-// to bf16 118 us a call = 2.33 PFLOP/s, 122 to 127 in the profiler; there 8192^3 467 us = 2.35, gradients of 4 x 4096^3 to bf16 246 to 255 us = 2.2 and
+// to bf16 118 us a call = 2.33 PFLOP/s, 122 to 127 in the profiler; there 8192^3 453 to 467 us = 2.43 to 2.35, gradients of 4 x 4096^3 to bf16 246 to 255 us = 2.2 and
 // to fp32 442 to 461 us = 1.2 PFLOP/s.  The matrix instructions are busy for 52, 56 and 63 % of the cycles (the first, the gradients), at 2 GHz; a
 // wavefront waits for loads, LDS and the others for a third of its time.  Four wavefronts of 128 x 128 a tile took 143 us where eight took 127, and
 // scales read earlier spill (317 us for 255 with b read down).  One row by 4096 x 4096 is bound by the reading of b and a launch: 6.2 us a call, 2.7 TB/s.
